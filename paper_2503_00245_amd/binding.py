@@ -1,4 +1,5 @@
-"""ctypes binding of libmoe_mi355x.so: the entry points of include/moe.h under the same names.
+"""ctypes binding of libmoe_mi355x.so: the entry points of include/moe.h and
+include/moe_quantised.h under the same names.
 
 Argument marshalling only: tensors are torch CUDA(HIP) tensors used for device memory
 and the current stream; every step of the layer runs in the library's kernels.  There
@@ -23,6 +24,9 @@ EXPORTS = ("moe_route", "moe_permute", "moe_expert_ffn", "moe_combine", "moe_for
            "moe_forward_static", "moe_stack_forward", "moe_forward_timed", "moe_workspace_bytes", "moe_status_string",
            "moe_expert_replacements", "moe_bles_workspace_bytes", "moe_bles_loss",
            "moe_offload_counters", "moe_delta_uniform")
+QUANTISED_EXPORTS = ("moe_route_scored", "moe_route_scored_backward", "moe_mxfp4_quantize", "moe_mxfp4_dequantize",
+                     "moe_mxfp4_packed_bytes", "moe_mxfp4_pack", "moe_mxfp4_workspace_bytes", "moe_mxfp4_experts",
+                     "moe_mxfp4_forward")  # include/moe_quantised.h
 
 
 class MoeShape(C.Structure):
@@ -32,6 +36,18 @@ class MoeShape(C.Structure):
 
 class MoeWeights(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in WEIGHT_FIELDS]
+
+
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+
+
+class RouteConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("score", "n_groups", "groups_kept", "group_top", "renormalize")] + \
+               [("scale", C.c_float)]
+
+
+class Mxfp4WeightsStruct(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("router_w", "router_b", "select_bias", "gate", "up", "down")]
 
 
 class MoeError(RuntimeError):
@@ -74,6 +90,21 @@ def lib() -> C.CDLL:
         L.moe_bles_loss.argtypes = [vp, vp, i32, i32, i32, i32, vp, vp, sz, vp]
         L.moe_offload_counters.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp]
         L.moe_delta_uniform.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, vp]
+        i64, rp, qp = C.c_int64, C.POINTER(RouteConfig), C.POINTER(Mxfp4WeightsStruct)
+        L.moe_route_scored.argtypes = [rp, i32, i32, i32, vp, vp, vp, vp, vp, vp]
+        L.moe_route_scored_backward.argtypes = [rp, i32, i32, i32, vp, vp, vp, vp, vp, vp]
+        L.moe_mxfp4_quantize.argtypes = [vp, i64, i32, i32, vp, vp, vp]
+        L.moe_mxfp4_dequantize.argtypes = [vp, vp, i64, i32, i32, vp, vp]
+        L.moe_mxfp4_packed_bytes.argtypes = [i32, i32, i32]
+        L.moe_mxfp4_packed_bytes.restype = sz
+        L.moe_mxfp4_pack.argtypes = [vp, vp, i32, i32, i32, vp, vp]
+        L.moe_mxfp4_workspace_bytes.argtypes = [sp]
+        L.moe_mxfp4_workspace_bytes.restype = sz
+        L.moe_mxfp4_experts.argtypes = [sp, qp, vp, vp, vp, vp, vp, sz, vp]
+        L.moe_mxfp4_forward.argtypes = [sp, rp, qp, vp, vp, vp, vp, vp, vp, sz, vp]
+        for fn in ("moe_route_scored", "moe_route_scored_backward", "moe_mxfp4_quantize", "moe_mxfp4_dequantize",
+                   "moe_mxfp4_pack", "moe_mxfp4_experts", "moe_mxfp4_forward"):
+            getattr(L, fn).restype = C.c_int
         for fn in ("moe_route", "moe_permute", "moe_expert_ffn", "moe_combine", "moe_forward",
                    "moe_forward_static", "moe_stack_forward", "moe_forward_timed", "moe_expert_replacements",
                    "moe_bles_loss", "moe_offload_counters", "moe_delta_uniform"):
@@ -256,3 +287,174 @@ def moe_delta_uniform(trace, n_experts: int, counts, delta, mean) -> None:
     L_, T, K = trace.shape
     _check("moe_delta_uniform", lib().moe_delta_uniform(
         _ptr(trace), L_, T, K, n_experts, _ptr(counts), _ptr(delta), _ptr(mean), _stream(trace.device)))
+
+
+# ---- routing from logits, and experts in microscaled 4-bit floating point (MXFP4) --------------------------------
+
+def make_route_config(score=SCORE_SOFTMAX, n_groups=1, groups_kept=1, group_top=1, renormalize=True,
+                      scale=1.0) -> RouteConfig:
+    return RouteConfig(score, n_groups, groups_kept, group_top, int(renormalize), scale)
+
+
+def _want(name: str, t: torch.Tensor, dtype, *shape) -> torch.Tensor:
+    """t, if it has this type and shape: the library takes pointers and cannot tell."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} must have shape {list(shape)}, got {list(t.shape)}")
+    return t
+
+
+def _same_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> None:
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError(f"tensors on {first.device} and {t.device}")
+
+
+def moe_route_scored(config: RouteConfig, logits, select_bias, topk_idx, topk_gate, scores=None) -> None:
+    """logits f32 [T,E], select_bias f32 [E] or None; topk_idx int32 [T,k], topk_gate f32 [T,k] and scores f32 [T,E]
+    (or None): outputs."""
+    T, E = logits.shape
+    k = topk_idx.shape[-1]
+    _want("logits", logits, torch.float32, T, E)
+    _want("topk_idx", topk_idx, torch.int32, T, k)
+    _want("topk_gate", topk_gate, torch.float32, T, k)
+    if select_bias is not None:
+        _want("select_bias", select_bias, torch.float32, E)
+    if scores is not None:
+        _want("scores", scores, torch.float32, T, E)
+    _same_device(logits, select_bias, topk_idx, topk_gate, scores)
+    _check("moe_route_scored", lib().moe_route_scored(
+        C.byref(config), T, E, k, _ptr(logits), _ptr(select_bias), _ptr(topk_idx), _ptr(topk_gate), _ptr(scores),
+        _stream(logits.device)))
+
+
+def moe_route_scored_backward(config: RouteConfig, logits, topk_idx, grad_gate, grad_scores, grad_logits) -> None:
+    """logits f32 [T,E], topk_idx int32 [T,k] of the forward call, grad_gate f32 [T,k], grad_scores f32 [T,E] or None;
+    grad_logits f32 [T,E]: output."""
+    T, E = logits.shape
+    k = topk_idx.shape[-1]
+    _want("logits", logits, torch.float32, T, E)
+    _want("topk_idx", topk_idx, torch.int32, T, k)
+    _want("grad_gate", grad_gate, torch.float32, T, k)
+    if grad_scores is not None:
+        _want("grad_scores", grad_scores, torch.float32, T, E)
+    _want("grad_logits", grad_logits, torch.float32, T, E)
+    _same_device(logits, topk_idx, grad_gate, grad_scores, grad_logits)
+    _check("moe_route_scored_backward", lib().moe_route_scored_backward(
+        C.byref(config), T, E, k, _ptr(logits), _ptr(topk_idx), _ptr(grad_gate), _ptr(grad_scores), _ptr(grad_logits),
+        _stream(logits.device)))
+
+
+def _mxfp4_rows(x, codes, scales):
+    cols = x.shape[-1]
+    _want("codes", codes, torch.uint8, *x.shape[:-1], cols // 2)
+    _want("scales", scales, torch.uint8, *x.shape[:-1], (cols + 31) // 32)
+    _same_device(x, codes, scales)
+    return x.numel() // max(cols, 1), cols
+
+
+def moe_mxfp4_quantize(x, codes, scales) -> None:
+    """x f32 or bf16 [..., C]; codes uint8 [..., C/2] and scales uint8 [..., ceil(C/32)]: outputs."""
+    rows, cols = _mxfp4_rows(x, codes, scales)
+    _check("moe_mxfp4_quantize", lib().moe_mxfp4_quantize(_ptr(x), rows, cols, _act_dtype(x), _ptr(codes), _ptr(scales),
+                                                          _stream(x.device)))
+
+
+def moe_mxfp4_dequantize(codes, scales, x) -> None:
+    """codes uint8 [..., C/2], scales uint8 [..., ceil(C/32)]; x f32 or bf16 [..., C]: output."""
+    rows, cols = _mxfp4_rows(x, codes, scales)
+    _check("moe_mxfp4_dequantize", lib().moe_mxfp4_dequantize(_ptr(codes), _ptr(scales), rows, cols, _act_dtype(x), _ptr(x),
+                                                              _stream(x.device)))
+
+
+def moe_mxfp4_pack(codes, scales) -> torch.Tensor:
+    """Matrices codes uint8 [E,R,C/2], scales uint8 [E,R,ceil(C/32)] in the layout that moe_mxfp4_experts reads."""
+    E, R, half = codes.shape
+    C_ = half * 2
+    _want("codes", codes, torch.uint8, E, R, half)
+    _want("scales", scales, torch.uint8, E, R, (C_ + 31) // 32)
+    _same_device(codes, scales)
+    n = int(lib().moe_mxfp4_packed_bytes(E, R, C_))
+    if n == 0:
+        raise MoeError("moe_mxfp4_packed_bytes", -2)
+    packed = torch.empty(n, dtype=torch.uint8, device=codes.device)
+    _check("moe_mxfp4_pack", lib().moe_mxfp4_pack(_ptr(codes), _ptr(scales), E, R, C_, _ptr(packed), _stream(codes.device)))
+    return packed
+
+
+class Mxfp4Weights:
+    """Packed weights of one layer, the tensors that hold them and their sizes."""
+
+    def __init__(self, E: int, d: int, F: int, tensors: Dict[str, Optional[torch.Tensor]]):
+        self.E, self.d, self.F, self.tensors = E, d, F, tensors
+        self.struct = Mxfp4WeightsStruct()
+        for name, t in tensors.items():
+            setattr(self.struct, name, _ptr(t))
+
+
+def make_mxfp4_weights(weights: Dict[str, Optional[torch.Tensor]]) -> Mxfp4Weights:
+    """weights: gate_codes, up_codes uint8 [E,F,d/2] and gate_scales, up_scales [E,F,ceil(d/32)], down_codes
+    [E,d,F/2] and down_scales [E,d,ceil(F/32)]; for moe_mxfp4_forward router_w f32 [E,d], and router_b and
+    select_bias f32 [E] or None."""
+    E, F, half = weights["gate_codes"].shape
+    d = half * 2
+    _want("up_codes", weights["up_codes"], torch.uint8, E, F, half)
+    _want("down_codes", weights["down_codes"], torch.uint8, E, d, F // 2)
+    t: Dict[str, Optional[torch.Tensor]] = {n: moe_mxfp4_pack(weights[n + "_codes"], weights[n + "_scales"])
+                                            for n in ("gate", "up", "down")}
+    for name, shape in (("router_w", (E, d)), ("router_b", (E,)), ("select_bias", (E,))):
+        t[name] = weights.get(name)
+        if t[name] is not None:
+            _want(name, t[name], torch.float32, *shape)
+    _same_device(*[v for v in t.values() if v is not None])
+    return Mxfp4Weights(E, d, F, t)
+
+
+def moe_mxfp4_workspace_bytes(shape: MoeShape) -> int:
+    return int(lib().moe_mxfp4_workspace_bytes(C.byref(shape)))
+
+
+def alloc_mxfp4_workspace(shape: MoeShape, device) -> torch.Tensor:
+    n = moe_mxfp4_workspace_bytes(shape)
+    if n == 0:
+        raise MoeError("moe_mxfp4_workspace_bytes", -1)
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+_DTYPES = {MOE_F32: torch.float32, MOE_BF16: torch.bfloat16}
+
+
+def _mxfp4_call(shape: MoeShape, weights: Mxfp4Weights, x, y, topk_idx, topk_gate, workspace) -> None:
+    if (shape.n_experts, shape.d_model, shape.d_ff) != (weights.E, weights.d, weights.F):
+        raise ValueError(f"shape of {shape.n_experts} experts {shape.d_model} / {shape.d_ff}, weights of "
+                         f"{weights.E} experts {weights.d} / {weights.F}")
+    T, k, dtype = shape.n_tokens, shape.top_k, _DTYPES.get(shape.act_dtype)
+    _want("x", x, dtype, T, shape.d_model)
+    _want("y", y, dtype, T, shape.d_model)
+    if topk_idx is not None:
+        _want("topk_idx", topk_idx, torch.int32, T, k)
+    if topk_gate is not None:
+        _want("topk_gate", topk_gate, torch.float32, T, k)
+    _same_device(x, y, topk_idx, topk_gate, workspace, weights.tensors["gate"])
+
+
+def moe_mxfp4_experts(shape: MoeShape, weights: Mxfp4Weights, x, topk_idx, topk_gate, y, workspace) -> None:
+    """The layer from the picks on: x [T,d], topk_idx int32 [T,k], topk_gate f32 [T,k]; y [T,d]: output."""
+    _mxfp4_call(shape, weights, x, y, topk_idx, topk_gate, workspace)
+    _check("moe_mxfp4_experts", lib().moe_mxfp4_experts(
+        C.byref(shape), C.byref(weights.struct), _ptr(x), _ptr(topk_idx), _ptr(topk_gate), _ptr(y), _ptr(workspace),
+        workspace.numel() * workspace.element_size(), _stream(x.device)))
+
+
+def moe_mxfp4_forward(shape: MoeShape, config: RouteConfig, weights: Mxfp4Weights, x, y, topk_idx=None, topk_gate=None,
+                      logits=None, workspace=None) -> None:
+    """Router, picks and experts: x [T,d]; y [T,d], and topk_idx, topk_gate, logits f32 [T,E] or None: outputs."""
+    _mxfp4_call(shape, weights, x, y, topk_idx, topk_gate, workspace)
+    if logits is not None:
+        _want("logits", logits, torch.float32, shape.n_tokens, shape.n_experts)
+        _same_device(x, logits)
+    _check("moe_mxfp4_forward", lib().moe_mxfp4_forward(
+        C.byref(shape), C.byref(config), C.byref(weights.struct), _ptr(x), _ptr(y), _ptr(topk_idx), _ptr(topk_gate),
+        _ptr(logits), _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+        _stream(x.device)))

@@ -1,0 +1,244 @@
+"""Experts in microscaled 4-bit floating point, on the GPU, against plain implementations in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2503_00245_amd as pkg
+from tests import operators_oracle as oo
+
+pytestmark = pytest.mark.gpu
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def dev():
+    return torch.device("cuda:0")
+
+
+def _quantize(x):
+    rows, cols = x.shape
+    codes = torch.full((rows, cols // 2), 0xAA, dtype=torch.uint8, device=x.device)
+    scales = torch.full((rows, -(-cols // 32)), 0xAA, dtype=torch.uint8, device=x.device)
+    pkg.moe_mxfp4_quantize(x, codes, scales)
+    return codes, scales
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(1, 8), (1, 32), (3, 40), (7, 72), (5, 432), (64, 256), (33, 1064), (130, 2048), (1001, 24), (0, 64)])
+def test_quantize_there_and_back(rows, cols, dtype):
+    rng = np.random.default_rng(rows * 1000 + cols)
+    x = rng.standard_normal((rows, cols)) * np.exp(3 * rng.standard_normal((rows, 1)))
+    x = torch.from_numpy(x.astype(np.float32)).to(DTYPES[dtype]).to(dev())
+    codes, scales = _quantize(x)
+    c, b = oo.quantize(x.double().cpu().numpy().reshape(rows, cols)) if rows else (np.zeros((0, cols), np.uint8), np.zeros((0, cols // 32), np.uint8))
+    assert np.array_equal(codes.cpu().numpy(), oo.pack_nibbles(c))
+    assert np.array_equal(scales.cpu().numpy(), b)
+    for back in DTYPES.values():
+        y = torch.full((rows, cols), float("nan"), dtype=back, device=dev())
+        pkg.moe_mxfp4_dequantize(codes, scales, y)
+        assert np.array_equal(y.double().cpu().numpy(), oo.values(c, b))  # exact: no tolerance
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_quantize_borders_and_ends_of_the_range(dtype):
+    # every border of the grid and its neighbours, at scales over the whole exponent range
+    m = np.concatenate([oo.GRID, oo.BORDERS, [7.0, 7.9375]])
+    block = np.zeros(32)
+    block[:len(m)] = m
+    block[len(m):2 * len(m) if 2 * len(m) <= 32 else 32] = -m[:32 - len(m)]
+    rows = [block * 2.0 ** e for e in (-125, -60, -1, 0, 1, 60, 124)]
+    near = block.copy()
+    near[1:16] *= 1 + 2.0 ** (-7 if dtype == "bf16" else -23)
+    rows += [near, np.zeros(32), -np.zeros(32)]
+    tiny = np.zeros(32)
+    tiny[:4] = [2.0 ** -126, 2.0 ** -130, -2.0 ** -128, 2.0 ** -133]  # subnormal numbers, scale byte 0
+    rows += [tiny]
+    for bad in (np.nan, np.inf, -np.inf):
+        r = np.ones(32)
+        r[5] = bad
+        rows.append(r)
+    x = torch.from_numpy(np.array(rows)).to(DTYPES[dtype]).to(dev())
+    codes, scales = _quantize(x)
+    c, b = oo.quantize(x.double().cpu().numpy())
+    got_c, got_b = codes.cpu().numpy(), scales.cpu().numpy()
+    fine = b[:, 0] != 255
+    assert np.array_equal(got_b, b)
+    assert np.array_equal(got_c[fine], oo.pack_nibbles(c)[fine])
+    y = torch.empty_like(x)
+    pkg.moe_mxfp4_dequantize(codes, scales, y)
+    y = y.double().cpu().numpy()
+    assert np.array_equal(y[fine], oo.values(c, b)[fine])
+    assert np.isnan(y[~fine]).all()
+
+
+def test_dequantize_every_code_at_every_scale():
+    code = np.tile(np.arange(16, dtype=np.uint8), 2)[None].repeat(256, 0)
+    b = np.arange(256, dtype=np.uint8)[:, None]
+    y = torch.empty(256, 32, device=dev())
+    pkg.moe_mxfp4_dequantize(torch.from_numpy(oo.pack_nibbles(code)).to(dev()), torch.from_numpy(b).to(dev()), y)
+    with np.errstate(over="ignore"):
+        want = oo.values(code, b).astype(np.float32)
+    got = y.cpu().numpy()
+    assert np.array_equal(got, want, equal_nan=True)
+
+
+def _matrices(rng, E, rows, cols, std):
+    code, b = oo.quantize((rng.standard_normal((E * rows, cols)) * std))
+    codes = torch.from_numpy(oo.pack_nibbles(code).reshape(E, rows, cols // 2)).to(dev())
+    scales = torch.from_numpy(b.reshape(E, rows, -1)).to(dev())
+    return codes, scales, oo.values(code, b).reshape(E, rows, cols)
+
+
+def _layer(rng, E, d, F):
+    w = {}
+    exact = []
+    for name, rows, cols in (("gate", F, d), ("up", F, d), ("down", d, F)):
+        w[name + "_codes"], w[name + "_scales"], v = _matrices(rng, E, rows, cols, 1.0 / np.sqrt(cols))
+        exact.append(v)
+    return w, exact
+
+
+def _picks(rng, T, E, k, skew):
+    p = -skew * np.log(np.arange(1, E + 1)) + rng.gumbel(size=(T, E))
+    idx = np.argsort(-p, axis=1)[:, :k].astype(np.int32)
+    gate = rng.random((T, k)).astype(np.float32)
+    return idx, gate / gate.sum(1, keepdims=True)
+
+
+def _run(x, w, idx, gate, E, k, d, F, dtype, residual, weights=None):
+    T = x.shape[0]
+    shape = pkg.make_shape(T, d, F, E, k, act_dtype=pkg.MOE_BF16 if dtype == "bf16" else pkg.MOE_F32,
+                           flags=pkg.FLAG_RESIDUAL if residual else 0)
+    weights = weights or pkg.make_mxfp4_weights(w)
+    # memory around the result and the workspace, and what the workspace held, play no part
+    n = pkg.moe_mxfp4_workspace_bytes(shape)
+    ws = torch.full((n + 512,), 0xFF, dtype=torch.uint8, device=dev())
+    y = torch.full((T + 2, d), 777.0, dtype=x.dtype, device=dev())
+    pkg.moe_mxfp4_experts(shape, weights, x, idx, gate, y[1:T + 1], ws[256:256 + n])
+    assert (y[0] == 777.0).all() and (y[T + 1] == 777.0).all()
+    assert (ws[:256] == 0xFF).all() and (ws[256 + n:] == 0xFF).all()
+    return y[1:T + 1]
+
+
+SHAPES = [  # T, d, F, E, k, skew
+    (1, 8, 8, 1, 1, 0), (1, 64, 64, 4, 2, 0), (1, 256, 512, 8, 2, 0), (1, 432, 1152, 8, 2, 0), (1, 520, 264, 64, 8, 0), (2, 256, 256, 8, 2, 0),
+    (3, 40, 72, 3, 3, 0), (5, 400, 1064, 8, 2, 1), (16, 512, 776, 4, 4, 0), (17, 264, 300 // 4 * 4, 5, 2, 0), (24, 1024, 512, 16, 4, 0),
+    (33, 128, 256, 2, 1, 3), (40, 256, 2048, 8, 2, 1), (64, 640, 1728, 4, 1, 9), (100, 72, 40, 64, 6, 0), (130, 432, 1152, 8, 2, 1),
+    (257, 520, 328, 4, 2, 2), (300, 256, 256, 1, 1, 0), (513, 200, 456, 8, 3, 1), (1100, 136, 264, 8, 8, 0), (5000, 64, 96, 32, 2, 1),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,d,F,E,k,skew", [s for s in SHAPES if s[2] % 8 == 0])
+def test_experts(T, d, F, E, k, skew, dtype):
+    print("experts", T, d, F, E, k, skew, dtype, flush=True)
+    rng = np.random.default_rng(T * 7 + d + F)
+    w, exact = _layer(rng, E, d, F)
+    idx, gate = _picks(rng, T, E, k, skew)
+    x = torch.from_numpy(rng.standard_normal((T, d)).astype(np.float32)).to(DTYPES[dtype]).to(dev())
+    residual = T % 2 == 1
+    y = _run(x, w, torch.from_numpy(idx).to(dev()), torch.from_numpy(gate).to(dev()), E, k, d, F, dtype, residual)
+    ref, tol = oo.experts(x.double().cpu().numpy(), exact, idx, gate.astype(np.float64), residual, 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24)
+    err = np.abs(y.double().cpu().numpy() - ref)
+    assert np.isfinite(err).all()
+    assert (err <= tol).all(), (err / np.maximum(tol, 1e-300)).max()
+
+
+def test_experts_of_no_tokens_and_the_same_bits_twice():
+    rng = np.random.default_rng(3)
+    E, d, F, k = 4, 256, 512, 2
+    w, _ = _layer(rng, E, d, F)
+    weights = pkg.make_mxfp4_weights(w)
+    empty = torch.empty(0, d, dtype=torch.bfloat16, device=dev())
+    pkg.moe_mxfp4_experts(pkg.make_shape(0, d, F, E, k), weights, empty, torch.empty(0, k, dtype=torch.int32, device=dev()),
+                          torch.empty(0, k, device=dev()), empty.clone(), torch.empty(256, dtype=torch.uint8, device=dev()))
+    for T in (1, 3, 40, 400):
+        idx, gate = _picks(rng, T, E, k, 1)
+        x = torch.randn(T, d, device=dev()).bfloat16()
+        idx, gate = torch.from_numpy(idx).to(dev()), torch.from_numpy(gate).to(dev())
+        a = _run(x, w, idx, gate, E, k, d, F, "bf16", False, weights).clone()
+        b = _run(x, w, idx, gate, E, k, d, F, "bf16", False, weights)
+        assert torch.equal(a, b)
+        # a token alone is what it is among others, but for the roundings of what is stored in between
+        one = _run(x[:1].contiguous(), w, idx[:1].contiguous(), gate[:1].contiguous(), E, k, d, F, "bf16", False, weights)
+        scale = a[:1].float().abs().max()
+        assert ((one - a[:1]).float().abs() <= 2.0 ** -6 * scale).all()
+
+
+def test_a_token_of_nan_stays_alone_and_bad_picks_stay_inside():
+    rng = np.random.default_rng(4)
+    E, d, F, k = 4, 256, 512, 2
+    w, exact = _layer(rng, E, d, F)
+    for T in (1, 20, 300):
+        idx, gate = _picks(rng, T, E, k, 0)
+        x = torch.randn(T, d, device=dev()).bfloat16()
+        bad = x.clone()
+        bad[T // 2, 7] = float("nan")
+        i, g = torch.from_numpy(idx).to(dev()), torch.from_numpy(gate).to(dev())
+        a, b = (_run(v, w, i, g, E, k, d, F, "bf16", False) for v in (x, bad))
+        others = [t for t in range(T) if t != T // 2]
+        assert torch.equal(a[others], b[others])
+        assert torch.isnan(b[T // 2]).all()
+        i2 = i.clone()
+        i2[T // 2] = torch.tensor([-5, E + 3], dtype=torch.int32, device=dev())
+        c = _run(x, w, i2, g, E, k, d, F, "bf16", False)
+        assert torch.equal(a[others], c[others])
+
+
+@pytest.mark.parametrize("T", [1, 3, 50, 600])
+def test_forward_is_its_stages(T):
+    rng = np.random.default_rng(T)
+    E, d, F, k = 16, 264, 320, 4
+    w, _ = _layer(rng, E, d, F)
+    w["router_w"] = torch.from_numpy(rng.standard_normal((E, d)).astype(np.float32) * 0.1).to(dev())
+    w["router_b"] = torch.from_numpy(rng.standard_normal(E).astype(np.float32)).to(dev())
+    w["select_bias"] = torch.from_numpy(rng.standard_normal(E).astype(np.float32) * 0.1).to(dev())
+    weights = pkg.make_mxfp4_weights(w)
+    x = torch.from_numpy(rng.standard_normal((T, d)).astype(np.float32)).to(dev()).bfloat16()
+    cfg = pkg.make_route_config(pkg.SCORE_SIGMOID, 4, 2, 2, True, 1.5)
+    shape = pkg.make_shape(T, d, F, E, k, flags=pkg.FLAG_RESIDUAL)
+    ws = pkg.alloc_mxfp4_workspace(shape, dev())
+    idx, gate = torch.empty(T, k, dtype=torch.int32, device=dev()), torch.empty(T, k, device=dev())
+    logits = torch.empty(T, E, device=dev())
+    y, y2, y3 = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+    pkg.moe_mxfp4_forward(shape, cfg, weights, x, y, idx, gate, logits, ws)
+    exact = x.double().cpu() @ w["router_w"].double().cpu().T + w["router_b"].double().cpu()
+    bound = (d + 2) * 2.0 ** -24 * (x.double().cpu().abs() @ w["router_w"].double().cpu().abs().T + w["router_b"].double().cpu().abs())
+    assert ((logits.double().cpu() - exact).abs() <= bound).all()
+    idx2, gate2 = torch.empty_like(idx), torch.empty_like(gate)
+    pkg.moe_route_scored(cfg, logits, w["select_bias"], idx2, gate2)
+    assert torch.equal(idx, idx2) and torch.equal(gate, gate2)
+    pkg.moe_mxfp4_experts(shape, weights, x, idx, gate, y2, ws)
+    assert torch.equal(y, y2)
+    pkg.moe_mxfp4_forward(shape, cfg, weights, x, y3, workspace=ws)
+    assert torch.equal(y, y3)
+
+
+@pytest.mark.parametrize("T", [1, 12, 200])
+def test_capture_and_another_stream(T):
+    rng = np.random.default_rng(T + 9)
+    E, d, F, k = 8, 256, 512, 2
+    w, _ = _layer(rng, E, d, F)
+    w["router_w"] = torch.from_numpy(rng.standard_normal((E, d)).astype(np.float32) * 0.1).to(dev())
+    weights = pkg.make_mxfp4_weights(w)
+    x = torch.randn(T, d, device=dev()).bfloat16()
+    cfg = pkg.make_route_config(pkg.SCORE_SOFTMAX)
+    shape = pkg.make_shape(T, d, F, E, k)
+    ws = pkg.alloc_mxfp4_workspace(shape, dev())
+    y, want = torch.empty_like(x), torch.empty_like(x)
+    pkg.moe_mxfp4_forward(shape, cfg, weights, x, want, workspace=ws)
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        pkg.moe_mxfp4_forward(shape, cfg, weights, x, y, workspace=ws)
+    stream.synchronize()
+    assert torch.equal(y, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        pkg.moe_mxfp4_forward(shape, cfg, weights, x, y, workspace=ws)
+    for _ in range(4):  # replays, with new inputs and eager calls between them
+        x.copy_(torch.randn(T, d, device=dev()))
+        pkg.moe_mxfp4_forward(shape, cfg, weights, x, want, workspace=ws)
+        y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want)
