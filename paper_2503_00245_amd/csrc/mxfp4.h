@@ -50,6 +50,23 @@ __device__ __forceinline__ unsigned mx_codes8(const float (&v)[8], int b) {
 #endif
 }
 
+// A lane's 32 values of a row, quantised: the operand of a k-step and its scale
+template <typename T>
+__device__ __forceinline__ void mx_quantise_32(const typename Store<T>::vec_t (&v)[32 / Store<T>::VEC], i32x4& codes, int& scale) {
+    typedef Store<T> S;
+    unsigned m = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) m = max(m, (unsigned)__float_as_int(S::get(v[i / S::VEC], i % S::VEC)) & 0x7fffffffu);
+    scale = mx_scale_byte(m);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        float f[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = S::get(v[(w * 8 + i) / S::VEC], (w * 8 + i) % S::VEC);
+        codes[w] = (int)mx_codes8(f, scale);
+    }
+}
+
 // Eight codes as the values that they stand for; scale byte 255: NaN
 __device__ __forceinline__ void mx_values8(unsigned codes, int b, float (&v)[8]) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -70,6 +87,33 @@ __device__ __forceinline__ unsigned mx_abs_max(const float (&v)[8]) {
     return m;
 }
 
+// Eight hidden columns (columns 32 fb + 8 (lane / 16) ..., row lane % 16 of tile n of block sb), quantised, into a matrix of `units`
+// units a block: a dword of codes a lane, and a byte of scale for four lanes.
+__device__ __forceinline__ void mx_store_hidden(const float (&f)[8], char* __restrict__ codes, char* __restrict__ scales, int units, int sb, int n, int fb, int lane) {
+    int m = (int)mx_abs_max(f);
+    m = max(m, __shfl_xor(m, 16, kWave));
+    m = max(m, __shfl_xor(m, 32, kWave));
+    const int b = mx_scale_byte(m), c = fb >> 2, at = (fb & 3) * 16 + (lane & 15);
+    const size_t unit = (size_t)sb * units + (c >> 1);
+    *reinterpret_cast<unsigned*>(codes + unit * kMxCodes + ((c & 1) * 2 + n) * 1024 + at * 16 + (lane >> 4) * 4) = mx_codes8(f, b);
+    if (lane < 16) scales[unit * kMxScales + at * 4 + (c & 1) * 2 + n] = (char)b;
+}
+// The same of a product that is not quantised: eight neighbours of row 32 sb + 16 n + lane % 16 of [.., N]
+template <typename T>
+__device__ __forceinline__ void mx_store_rows(const float (&f)[8], char* __restrict__ out, int N, int sb, int n, int fb, int lane) {
+    const int col = fb * 32 + (lane >> 4) * 8;
+    if (col >= N) return;
+    T* y = reinterpret_cast<T*>(out) + ((size_t)sb * 32 + n * 16 + (lane & 15)) * N + col;
+    typedef typename Store<T>::vec_t vec_t;
+#pragma unroll
+    for (int h = 0; h < 8; h += Store<T>::VEC) {
+        vec_t o;
+#pragma unroll
+        for (int j = 0; j < Store<T>::VEC; ++j) o[j] = Store<T>::from_f32(f[h + j]);
+        *reinterpret_cast<vec_t*>(y + h) = o;
+    }
+}
+
 // D (16 x 16, fp32) += A (16 x 128) B^T; SA, SB: which byte of the dwords sa, sb scales the lane's 32 codes
 template <int SA, int SB>
 __device__ __forceinline__ f32x4 mx_mfma(const i32x4& a, const i32x4& b, const f32x4& c, int sa, int sb) {
@@ -82,14 +126,38 @@ __device__ __forceinline__ f32x4 mx_mfma(const i32x4& a, const i32x4& b, const f
 #endif
 }
 
+// A unit: 32 rows of weights (tiles t of the first index) by 32 of activations.  w, x: [k-step][tile]
+__device__ __forceinline__ void mx_unit(f32x4 (&acc)[2][2], const i32x4 (&w)[2][2], const i32x4 (&x)[2][2], int sw, int sx) {
+    acc[0][0] = mx_mfma<0, 0>(w[0][0], x[0][0], acc[0][0], sw, sx);
+    acc[0][1] = mx_mfma<0, 1>(w[0][0], x[0][1], acc[0][1], sw, sx);
+    acc[1][0] = mx_mfma<1, 0>(w[0][1], x[0][0], acc[1][0], sw, sx);
+    acc[1][1] = mx_mfma<1, 1>(w[0][1], x[0][1], acc[1][1], sw, sx);
+    acc[0][0] = mx_mfma<2, 2>(w[1][0], x[1][0], acc[0][0], sw, sx);
+    acc[0][1] = mx_mfma<2, 3>(w[1][0], x[1][1], acc[0][1], sw, sx);
+    acc[1][0] = mx_mfma<3, 2>(w[1][1], x[1][0], acc[1][0], sw, sx);
+    acc[1][1] = mx_mfma<3, 3>(w[1][1], x[1][1], acc[1][1], sw, sx);
+}
+
 // ---- launchers ---------------------------------------------------------------------------------------
 struct MxLayout {  // byte offsets of a workspace; every region starts 256-byte aligned
-    size_t idx, gate, logits, slot, starts, xq, hq, y, total;
+    size_t idx, gate, logits, slot, starts, offsets, perm, sort, xq, hq, y, total;
     int blocks;    // blocks of 32 rows that hold the pairs of all experts, each expert's from a block of its own
 };
 MxLayout mx_layout(const moe_shape& s);
 int launch_mx_experts(const moe_shape& s, const moe_mxfp4_weights& w, const void* x, const int32_t* idx, const float* gate, void* y,
                       const MxLayout& l, char* ws, hipStream_t st);
+// Few pairs: two launches, without a dispatch (mxfp4_few.hip).  Whole layer, us, in these / in four launches: 2048 / 5632, 2 of 8 experts: one token
+// 14.7 / 20.3, two 20.4 / 23.9, four 35.3 / 37.0, eight 42.5 / 42.3; 1024 / 2816, 4 of 16 experts, four tokens 27.2 / 22.3.
+constexpr int kMxFewPairs = 8;
+inline bool mx_few(const moe_shape& s) { return (long long)s.n_tokens * s.top_k <= kMxFewPairs; }
+int launch_mx_few(const moe_shape& s, const moe_mxfp4_weights& w, const void* x, const int32_t* idx, const float* gate, void* y, const MxLayout& l, char* ws,
+                  hipStream_t st);
+// Products of some rows an expert (mxfp4_stream.hip), the same arguments
+int launch_mx_stream(bool swiglu, int act_dtype, const void* w0, const void* w1, const char* a, char* out, const int32_t* starts, int P, int E,
+                     int all_blocks, int N, int K, hipStream_t st);
+// Products of many rows (mxfp4_gemm.hip): swiglu: hidden rows (w0 gate, w1 up), else rows of act_dtype (w0).  bs: rows of a tile, 256, 128 or 64
+int launch_mx_gemm(bool swiglu, int act_dtype, const void* w0, const void* w1, const char* a, char* out, const int32_t* starts, int P, int E,
+                   int all_blocks, int N, int K, int bs, hipStream_t st);
 int launch_router_logits(const moe_shape& s, const void* x, const float* rw, const float* rb, float* logits, hipStream_t st);
 int launch_route_scored(const moe_route_config& c, int T, int E, int k, const float* logits, const float* bias, int32_t* idx, float* gate,
                         float* scores, hipStream_t st);

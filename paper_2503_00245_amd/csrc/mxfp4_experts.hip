@@ -5,6 +5,7 @@
 // its own, in the layout of mxfp4.h; the order inside an expert does not matter to any result.
 #include <algorithm>
 
+#include "gemm.h"
 #include "mxfp4.h"
 
 namespace moe {
@@ -13,163 +14,81 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// ---- dispatch: the first block of every expert, and every pair's row -------------------------------------
-constexpr int kDispatchThreads = 1024;
-__global__ __launch_bounds__(kDispatchThreads) void mx_dispatch_kernel(const int32_t* __restrict__ idx, int P, int E, int32_t* __restrict__ starts,
-                                                                       int32_t* __restrict__ slot) {
-    __shared__ int s_count[kMaxExperts], s_next[kMaxExperts];
-    if (threadIdx.x < kMaxExperts) s_count[threadIdx.x] = 0;
-    __syncthreads();
-    for (int p = threadIdx.x; p < P; p += kDispatchThreads) {
-        const unsigned e = (unsigned)idx[p];
-        if (e < (unsigned)E) atomicAdd(&s_count[e], 1);
-    }
-    __syncthreads();
-    if (threadIdx.x < kWave) {
-        const int e = threadIdx.x, n = e < E ? mx_blocks(s_count[e]) : 0;
-        const int end = wave_scan(n);
-        s_next[e] = (end - n) * 32;
-        if (e < E) starts[e] = end - n;
-        if (e == E - 1) starts[E] = end;
-    }
-    __syncthreads();
-    for (int p = threadIdx.x; p < P; p += kDispatchThreads) {
-        const unsigned e = (unsigned)idx[p];
-        slot[p] = e < (unsigned)E ? atomicAdd(&s_next[e], 1) : -1;
-    }
-}
-
-// ---- rows of the tokens, quantised, to the rows of their pairs ----------------------------------------------
-// A wave takes 512 columns of a token: eight values a lane, four lanes a scale.
+// ---- rows of the experts, quantised --------------------------------------------------------------------------
+// A workgroup makes one block of 32 rows.  Up to kMxKeyPairs pairs it finds the expert of its block and the pairs of its rows
+// from all picks itself (PairKeys); beyond, from the sorted pairs (perm, offsets).  A lane takes the 32 values of a
+// row that share a scale, so that nothing is exchanged and the block leaves in runs of 1 KB.
+constexpr int kRowThreads = 512, kRowWaves = kRowThreads / kWave;
+constexpr int kMxKeyPairs = kKeyChunks * 4 * kRowThreads;
 template <typename T>
-__global__ __launch_bounds__(kThreads) void mx_rows_kernel(const T* __restrict__ x, const int32_t* __restrict__ slot, int T_, int k, int d, int units,
-                                                           char* __restrict__ codes, char* __restrict__ scales) {
+__global__ __launch_bounds__(kRowThreads) void mx_rows_kernel(const T* __restrict__ x, const int32_t* __restrict__ idx, const int32_t* __restrict__ perm,
+                                                              const int32_t* __restrict__ offsets, int P, int E, int k, int d, int32_t* __restrict__ starts,
+                                                              int32_t* __restrict__ slot, char* __restrict__ codes, char* __restrict__ scales) {
     typedef Store<T> S;
-    const int lane = threadIdx.x & 63;
-    const int t = blockIdx.x;
-    for (int i = threadIdx.x * 8; i < units * kMxUnit; i += kThreads * 8) {
-        float f[8];
-#pragma unroll
-        for (int q = 0; q < 8; q += S::VEC) {
-            if (i < d) {
-                const typename S::vec_t v = *reinterpret_cast<const typename S::vec_t*>(x + (size_t)t * d + i + q);
-#pragma unroll
-                for (int j = 0; j < S::VEC; ++j) f[q + j] = S::get(v, j);
-            } else {
-#pragma unroll
-                for (int j = 0; j < S::VEC; ++j) f[q + j] = 0.f;
-            }
-        }
-        int m = (int)mx_abs_max(f);
-        m = max(m, dpp_i32<kDppSwap1>(m));
-        m = max(m, dpp_i32<kDppSwap2>(m));
-        const int b = mx_scale_byte(m);
-        const unsigned c8 = mx_codes8(f, b);
-        const int c = i >> 7, q = i >> 5 & 3;
-        for (int j = 0; j < k; ++j) {
-            const int r = slot[(size_t)t * k + j];
-            if (r < 0) continue;
-            const size_t unit = (size_t)(r >> 5) * units + (c >> 1);
-            const int tile = r >> 4 & 1, ln = q * 16 + (r & 15);
-            *reinterpret_cast<unsigned*>(codes + unit * kMxCodes + ((c & 1) * 2 + tile) * 1024 + ln * 16 + (lane & 3) * 4) = c8;
-            if ((lane & 3) == 0) scales[unit * kMxScales + ln * 4 + (c & 1) * 2 + tile] = (char)b;
-        }
+    constexpr int VECS = 32 / S::VEC;
+    __shared__ int s_count[kRowWaves][kMaxExperts], s_pair[32 + kWave];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), block = blockIdx.x;
+    const int units = mx_units(d);
+    int lo = 0, hi = 0;
+    PairKeys<kRowThreads> keys;
+    if (!perm) {
+        keys.load(idx, P);
+        keys.bounds(E, s_count, lo, hi);
+    } else if (lane < E) {
+        lo = offsets[lane];
+        hi = offsets[lane + 1];
     }
-}
-
-// ---- products ---------------------------------------------------------------------------------------------------
-// The expert of a block of rows
-__device__ __forceinline__ int expert_of(const int32_t* __restrict__ starts, int E, int block) {
-    int e = 0;
-    while (e < E - 1 && block >= starts[e + 1]) ++e;
-    return e;
-}
-
-// One wave: 32 output columns (with SWIGLU the same of gate and of up) of 32 rows, operands straight from memory.
-// SWIGLU: hidden rows, quantised again, in the layout of the next product; else rows of T.
-template <bool SWIGLU, typename T>
-__global__ __launch_bounds__(kThreads) void mx_product_kernel(const char* __restrict__ w0, const char* __restrict__ w1, const char* __restrict__ a,
-                                                              const int32_t* __restrict__ starts, int E, int all_blocks, int N, int K,
-                                                              char* __restrict__ out) {
-    const int lane = threadIdx.x & 63;
-    const int fb = blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6), sb = blockIdx.y;
-    const int units = mx_units(K), fbs = mx_blocks(N), out_units = mx_units(N);
-    if (sb >= starts[E]) return;
-    const int e = expert_of(starts, E, sb);
-    if (fb >= (SWIGLU ? out_units * (kMxUnit / 32) : fbs)) return;
-    const char* ac = a + (size_t)sb * units * kMxCodes;
-    const char* as = a + (size_t)all_blocks * units * kMxCodes + (size_t)sb * units * kMxScales;
-    constexpr int M = SWIGLU ? 2 : 1;
-    f32x4 acc[M][2][2];
-#pragma unroll
-    for (int m = 0; m < M; ++m)
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int n = 0; n < 2; ++n) acc[m][t][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (fb < fbs) {
-        const size_t at = ((size_t)e * fbs + fb) * units, all = (size_t)E * fbs * units * kMxCodes;
-        for (int u = 0; u < units; ++u) {
-            i32x4 fa[M][2][2], fx[2][2];
-            int sa[M];
-            const int sx = *reinterpret_cast<const int*>(as + (size_t)u * kMxScales + lane * 4);
-#pragma unroll
-            for (int m = 0; m < M; ++m) {
-                const char* w = m ? w1 : w0;
-                sa[m] = *reinterpret_cast<const int*>(w + all + (at + u) * kMxScales + lane * 4);
-#pragma unroll
-                for (int c = 0; c < 2; ++c)
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) fa[m][c][t] = *reinterpret_cast<const i32x4*>(w + (at + u) * kMxCodes + (c * 2 + t) * 1024 + lane * 16);
-            }
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-                for (int t = 0; t < 2; ++t) fx[c][t] = *reinterpret_cast<const i32x4*>(ac + (size_t)u * kMxCodes + (c * 2 + t) * 1024 + lane * 16);
-#pragma unroll
-            for (int m = 0; m < M; ++m) {
-                acc[m][0][0] = mx_mfma<0, 0>(fa[m][0][0], fx[0][0], acc[m][0][0], sa[m], sx);
-                acc[m][0][1] = mx_mfma<0, 1>(fa[m][0][0], fx[0][1], acc[m][0][1], sa[m], sx);
-                acc[m][1][0] = mx_mfma<1, 0>(fa[m][0][1], fx[0][0], acc[m][1][0], sa[m], sx);
-                acc[m][1][1] = mx_mfma<1, 1>(fa[m][0][1], fx[0][1], acc[m][1][1], sa[m], sx);
-                acc[m][0][0] = mx_mfma<2, 2>(fa[m][1][0], fx[1][0], acc[m][0][0], sa[m], sx);
-                acc[m][0][1] = mx_mfma<2, 3>(fa[m][1][0], fx[1][1], acc[m][0][1], sa[m], sx);
-                acc[m][1][0] = mx_mfma<3, 2>(fa[m][1][1], fx[1][0], acc[m][1][0], sa[m], sx);
-                acc[m][1][1] = mx_mfma<3, 3>(fa[m][1][1], fx[1][1], acc[m][1][1], sa[m], sx);
-            }
-        }
+    const int n_blocks = mx_blocks(hi - lo), end = wave_scan(n_blocks), start = end - n_blocks;
+    if (block == 0 && blockIdx.y == 0 && wave == 0) {
+        if (lane < E) starts[lane] = start;
+        if (lane == E - 1) starts[E] = end;
     }
-    // a lane holds columns 32 fb + 8 (lane / 16) .. + 8 of rows lane % 16 of both tiles
-#pragma unroll
-    for (int n = 0; n < 2; ++n) {
-        float f[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = SWIGLU ? silu_f32(acc[0][i / 4][n][i % 4]) * acc[M - 1][i / 4][n][i % 4] : acc[0][i / 4][n][i % 4];
-        if constexpr (SWIGLU) {
-            int m = (int)mx_abs_max(f);
-            m = max(m, __shfl_xor(m, 16, kWave));
-            m = max(m, __shfl_xor(m, 32, kWave));
-            const int b = mx_scale_byte(m);
-            const int c = fb >> 2, q = fb & 3, ln = q * 16 + (lane & 15);
-            const size_t unit = (size_t)sb * out_units + (c >> 1);
-            *reinterpret_cast<unsigned*>(out + unit * kMxCodes + ((c & 1) * 2 + n) * 1024 + ln * 16 + (lane >> 4) * 4) = mx_codes8(f, b);
-            if (lane < 16) out[(size_t)all_blocks * out_units * kMxCodes + unit * kMxScales + ln * 4 + (c & 1) * 2 + n] = (char)b;
-        } else {
-            const int col = fb * 32 + (lane >> 4) * 8;
-            if (col < N) {
-                T* y = reinterpret_cast<T*>(out) + ((size_t)sb * 32 + n * 16 + (lane & 15)) * N + col;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = Store<T>::from_f32(f[i]);
-            }
-        }
+    const unsigned long long at = __ballot(start <= block && block < end);
+    if (!at) return;
+    const int e = __ffsll((long long)at) - 1, first = (block - MOE_READLANE(start, e)) * 32;
+    const int e_lo = MOE_READLANE(lo, e), n = min(32, MOE_READLANE(hi, e) - e_lo - first);
+    if (!perm) {
+        keys.rows(e, first, n, 32, s_count, s_pair);
+    } else {
+        if (threadIdx.x < n) s_pair[threadIdx.x] = perm[e_lo + first + threadIdx.x];
+        __syncthreads();
     }
+    if (blockIdx.y == 0 && threadIdx.x < n) slot[s_pair[threadIdx.x]] = block * 32 + threadIdx.x;
+    const int u = blockIdx.y * kRowWaves + wave;
+    if (u >= units) return;
+    const int q = lane >> 4;
+    unsigned scale = 0;
+    typename S::vec_t v[4][VECS];
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct) {
+        const int p = s_pair[min(16 * (ct & 1) + (lane & 15), n - 1)];  // (rows past the last are the last one again)
+        const T* row = x + (size_t)quick_div(p, k) * d;
+        const int col = u * kMxUnit + (ct >> 1) * 128 + q * 32;
+#pragma unroll
+        for (int i = 0; i < VECS; ++i) v[ct][i] = *reinterpret_cast<const typename S::vec_t*>(row + min(col + i * S::VEC, d - S::VEC));
+    }
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct) {
+        const int col = u * kMxUnit + (ct >> 1) * 128 + q * 32;
+        if (col + 32 > d) {
+#pragma unroll
+            for (int i = 0; i < VECS; ++i)
+                if (col + i * S::VEC >= d) v[ct][i] = typename S::vec_t{};
+        }
+        i32x4 c;
+        int b;
+        mx_quantise_32<T>(v[ct], c, b);
+        *reinterpret_cast<i32x4*>(codes + ((size_t)block * units + u) * kMxCodes + ct * 1024 + lane * 16) = c;
+        scale |= (unsigned)b << (8 * ct);
+    }
+    *reinterpret_cast<unsigned*>(scales + ((size_t)block * units + u) * kMxScales + lane * 4) = scale;
 }
 
 // ---- combine --------------------------------------------------------------------------------------------------------
 // y_t = sum_j g_tj (row of pair (t, j)) (+ x_t), in fp32 and ascending j; a lane takes one 16-byte piece of a row.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void mx_combine_kernel(const T* __restrict__ rows, const int32_t* __restrict__ slot, const float* __restrict__ gate,
-                                                              const T* __restrict__ residual, T* __restrict__ y, int pieces, int k, long long all) {
+                                                              const T* __restrict__ residual, T* __restrict__ y, int pieces, int k, long long all, int last_row) {
     typedef Store<T> S;
     for (long long i = blockIdx.x * (long long)kThreads + threadIdx.x; i < all; i += gridDim.x * (long long)kThreads) {
         const long long t = i / pieces;
@@ -179,7 +98,7 @@ __global__ __launch_bounds__(kThreads) void mx_combine_kernel(const T* __restric
 #pragma unroll
         for (int q = 0; q < S::VEC; ++q) f[q] = 0.f;
         for (int j = 0; j < k; ++j) {
-            const int r = max(slot[t * k + j], 0);
+            const int r = min(max(slot[t * k + j], 0), last_row);  // (in range for picks of no expert as well)
             const float g = gate[t * k + j];
             const typename S::vec_t v = *reinterpret_cast<const typename S::vec_t*>(rows + r * d + at);
 #pragma unroll
@@ -214,11 +133,26 @@ MxLayout mx_layout(const moe_shape& s) {
     l.logits = take((size_t)s.n_tokens * s.n_experts * sizeof(float));
     l.slot = take(P * sizeof(int32_t));
     l.starts = take((s.n_experts + 1) * sizeof(int32_t));
+    l.offsets = take((s.n_experts + 1) * sizeof(int32_t));
+    l.perm = take(P > kMxKeyPairs ? P * sizeof(int32_t) : 0);
+    l.sort = take(P > kMxKeyPairs ? sizeof(int32_t) * 256 * s.n_experts : 0);  // (launch_permute: up to 256 counts an expert)
     l.xq = take((size_t)l.blocks * mx_units(s.d_model) * (kMxCodes + kMxScales));
     l.hq = take((size_t)l.blocks * mx_units(s.d_ff) * (kMxCodes + kMxScales));
     l.y = take((size_t)l.blocks * 32 * s.d_model * elt_size(s.act_dtype));
     l.total = cur;
     return l;
+}
+
+// Rows of a tile of either product; 32: mxfp4_stream.hip
+struct MxTiles {
+    int hidden, down;
+};
+static MxTiles mx_tiles(int P, int E, int d, int F) {
+    const int rows = P / E;
+    MxTiles t{32, 32};
+    if (rows >= 96) t = {128, 64};
+    if (rows >= 384) t = {256, 256};
+    return t;
 }
 
 template <typename T>
@@ -227,23 +161,35 @@ static int experts(const moe_shape& s, const moe_mxfp4_weights& w, const T* x, c
     const int P = s.n_tokens * s.top_k, E = s.n_experts, d = s.d_model, F = s.d_ff;
     int32_t* slot = reinterpret_cast<int32_t*>(ws + l.slot);
     int32_t* starts = reinterpret_cast<int32_t*>(ws + l.starts);
-    hipLaunchKernelGGL(mx_dispatch_kernel, dim3(1), dim3(kDispatchThreads), 0, st, idx, P, E, starts, slot);
-    hipLaunchKernelGGL(mx_rows_kernel<T>, dim3(s.n_tokens), dim3(kThreads), 0, st, x, slot, s.n_tokens, s.top_k, d, mx_units(d), ws + l.xq,
-                       ws + l.xq + (size_t)l.blocks * mx_units(d) * kMxCodes);
-    constexpr int W = kThreads / 64;
-    hipLaunchKernelGGL((mx_product_kernel<true, T>), dim3(mx_units(F) * (kMxUnit / 32) / W, l.blocks), dim3(kThreads), 0, st,
-                       static_cast<const char*>(w.gate), static_cast<const char*>(w.up), ws + l.xq, starts, E, l.blocks, F, d, ws + l.hq);
-    hipLaunchKernelGGL((mx_product_kernel<false, T>), dim3((mx_blocks(d) + W - 1) / W, l.blocks), dim3(kThreads), 0, st, static_cast<const char*>(w.down),
-                       (const char*)nullptr, ws + l.hq, starts, E, l.blocks, d, F, ws + l.y);
+    const int32_t *perm = nullptr, *offsets = nullptr;
+    if (P > kMxKeyPairs) {
+        int32_t* sorted = reinterpret_cast<int32_t*>(ws + l.perm);
+        const int rc = launch_permute(P, E, idx, reinterpret_cast<int32_t*>(ws + l.offsets), sorted, slot, ws + l.sort, l.xq - l.sort, st);
+        if (rc != MOE_OK) return rc;
+        perm = sorted;
+        offsets = reinterpret_cast<int32_t*>(ws + l.offsets);
+    }
+    const int units = mx_units(d);
+    hipLaunchKernelGGL(mx_rows_kernel<T>, dim3(l.blocks, (units + kRowWaves - 1) / kRowWaves), dim3(kRowThreads), 0, st, x, idx, perm, offsets, P, E, s.top_k, d,
+                       starts, slot, ws + l.xq, ws + l.xq + (size_t)l.blocks * units * kMxCodes);
+    const MxTiles tiles = mx_tiles(P, E, d, F);
+    auto product = [&](bool swiglu, int rows, const void* w0, const void* w1, char* a, char* out, int N, int K) {
+        return rows <= 32 ? launch_mx_stream(swiglu, s.act_dtype, w0, w1, a, out, starts, P, E, l.blocks, N, K, st)
+                          : launch_mx_gemm(swiglu, s.act_dtype, w0, w1, a, out, starts, P, E, l.blocks, N, K, rows, st);
+    };
+    int rc = product(true, tiles.hidden, w.gate, w.up, ws + l.xq, ws + l.hq, F, d);
+    if (rc == MOE_OK) rc = product(false, tiles.down, w.down, nullptr, ws + l.hq, ws + l.y, d, F);
+    if (rc != MOE_OK) return rc;
     const int pieces = d / Store<T>::VEC;
     const long long all = (long long)s.n_tokens * pieces;
     hipLaunchKernelGGL(mx_combine_kernel<T>, dim3((unsigned)std::min<long long>((all + kThreads - 1) / kThreads, 1 << 20)), dim3(kThreads), 0, st,
-                       reinterpret_cast<const T*>(ws + l.y), slot, gate, (s.flags & MOE_FLAG_RESIDUAL) ? x : nullptr, y, pieces, s.top_k, all);
+                       reinterpret_cast<const T*>(ws + l.y), slot, gate, (s.flags & MOE_FLAG_RESIDUAL) ? x : nullptr, y, pieces, s.top_k, all, l.blocks * 32 - 1);
     return launch_status();
 }
 
 int launch_mx_experts(const moe_shape& s, const moe_mxfp4_weights& w, const void* x, const int32_t* idx, const float* gate, void* y,
                       const MxLayout& l, char* ws, hipStream_t st) {
+    if (mx_few(s)) return launch_mx_few(s, w, x, idx, gate, y, l, ws, st);
     if (s.act_dtype == MOE_F32) return experts<float>(s, w, static_cast<const float*>(x), idx, gate, static_cast<float*>(y), l, ws, st);
     return experts<bf16_t>(s, w, static_cast<const bf16_t*>(x), idx, gate, static_cast<bf16_t*>(y), l, ws, st);
 }

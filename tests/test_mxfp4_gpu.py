@@ -121,14 +121,14 @@ def _run(x, w, idx, gate, E, k, d, F, dtype, residual, weights=None):
 
 SHAPES = [  # T, d, F, E, k, skew
     (1, 8, 8, 1, 1, 0), (1, 64, 64, 4, 2, 0), (1, 256, 512, 8, 2, 0), (1, 432, 1152, 8, 2, 0), (1, 520, 264, 64, 8, 0), (2, 256, 256, 8, 2, 0),
-    (3, 40, 72, 3, 3, 0), (5, 400, 1064, 8, 2, 1), (16, 512, 776, 4, 4, 0), (17, 264, 300 // 4 * 4, 5, 2, 0), (24, 1024, 512, 16, 4, 0),
+    (3, 40, 72, 3, 3, 0), (5, 400, 1064, 8, 2, 1), (16, 512, 776, 4, 4, 0), (17, 264, 304, 5, 2, 0), (32, 136, 520, 64, 8, 0), (32, 264, 72, 3, 2, 0), (24, 1024, 512, 16, 4, 0),
     (33, 128, 256, 2, 1, 3), (40, 256, 2048, 8, 2, 1), (64, 640, 1728, 4, 1, 9), (100, 72, 40, 64, 6, 0), (130, 432, 1152, 8, 2, 1),
     (257, 520, 328, 4, 2, 2), (300, 256, 256, 1, 1, 0), (513, 200, 456, 8, 3, 1), (1100, 136, 264, 8, 8, 0), (5000, 64, 96, 32, 2, 1),
 ]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("T,d,F,E,k,skew", [s for s in SHAPES if s[2] % 8 == 0])
+@pytest.mark.parametrize("T,d,F,E,k,skew", SHAPES)
 def test_experts(T, d, F, E, k, skew, dtype):
     print("experts", T, d, F, E, k, skew, dtype, flush=True)
     rng = np.random.default_rng(T * 7 + d + F)
@@ -242,3 +242,17 @@ def test_capture_and_another_stream(T):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("T,E,k", [(1, 3, 3), (5, 2, 2), (20, 8, 4), (32, 4, 4), (32, 16, 8), (60, 8, 4)])
+def test_an_expert_that_a_token_names_twice_counts_twice(T, E, k):
+    print("twice", T, E, k, flush=True)
+    d, F = 264, 328
+    rng = np.random.default_rng(T)
+    w, exact = _layer(rng, E, d, F)
+    idx = rng.integers(0, 2, (T, k)).astype(np.int32)  # two experts alone: more rows of each than there are tokens
+    gate = rng.random((T, k)).astype(np.float32)
+    x = torch.from_numpy(rng.standard_normal((T, d)).astype(np.float32)).to(dev()).bfloat16()
+    y = _run(x, w, torch.from_numpy(idx).to(dev()), torch.from_numpy(gate).to(dev()), E, k, d, F, "bf16", False)
+    ref, tol = oo.experts(x.double().cpu().numpy(), exact, idx, gate.astype(np.float64), False, 2.0 ** -8)
+    assert (np.abs(y.double().cpu().numpy() - ref) <= tol).all()
