@@ -4,6 +4,7 @@
 // The pairs (token, slot) of an expert are brought together in blocks of 32 rows, every expert's from a block of
 // its own, in the layout of mxfp4.h; the order inside an expert does not matter to any result.
 #include <algorithm>
+#include <cmath>
 
 #include "gemm.h"
 #include "mxfp4.h"
@@ -143,16 +144,27 @@ MxLayout mx_layout(const moe_shape& s) {
     return l;
 }
 
-// Rows of a tile of either product; 32: mxfp4_stream.hip
-struct MxTiles {
-    int hidden, down;
-};
-static MxTiles mx_tiles(int P, int E, int d, int F) {
-    const int rows = P / E;
-    MxTiles t{32, 32};
-    if (rows >= 96) t = {128, 64};
-    if (rows >= 384) t = {256, 256};
-    return t;
+// Rows of a tile of a product of P rows in E groups: 32 (mxfp4_stream.hip), 64, 128 or 256 (mxfp4_gemm.hip), whichever is the shortest by what
+// they measured, in us.  Tiles: rounds of 256 workgroups, a round so much a tile and so much a unit of K.  Streamed: so much of a CU for 32 rows of
+// weights by 32, or the weights at 4.6 TB/s (in tiles 3.5).  How unevenly the rows are spread the host does not know: half a tile more
+// an expert.  Whole layers, us, this choice / the best of eight pairs of choices: 2048 / 5632, 2 of 8 experts, 200 tokens 56.8 / 54.0, 400 63.8 / 63.8, 800
+// 75.5 / 75.5, 1200 94.1 / 89.6, 2048 132.2 / 132.2; 1024 / 2816, 256 tokens 24.2 / 23.9, 2048 55.2 / 55.2; 1440 / 3840, 777 tokens 51.9 / 51.9; 432 / 1152,
+// 300 tokens 15.9 / 15.9.
+static int mx_tile_rows(bool swiglu, int P, int E, int N, int K) {
+    const double rows = (double)P / E, units = mx_units(K), weights_mb = 0.53e-6 * N * (double)K * (swiglu ? 2 : 1) * std::min(P, E);
+    auto groups = [&](int of) { return std::min((double)P, E * std::max(1.0, rows / of + 0.5)); };
+    double best = std::max(mx_blocks(N) * groups(32) / 256 * (0.35 + units * (swiglu ? 0.10 : 0.08)), weights_mb / 4.6) + 3.0;
+    int choice = 32;
+    struct {
+        int rows;
+        double tile, unit;
+    } const tiles[] = {{64, swiglu ? 3.8 : 4.9, 0.55}, {128, 4.8, 0.85}, {256, swiglu ? 6.0 : 5.0, 1.52}};
+    for (const auto& t : tiles) {
+        const double rounds = std::ceil(groups(t.rows) * ((N + (swiglu ? 127 : 255)) / (swiglu ? 128 : 256)) / 256);
+        const double us = std::max(rounds * (t.tile + units * t.unit), weights_mb / 3.5) + 1.5;
+        if (us < best) best = us, choice = t.rows;
+    }
+    return choice;
 }
 
 template <typename T>
@@ -172,13 +184,13 @@ static int experts(const moe_shape& s, const moe_mxfp4_weights& w, const T* x, c
     const int units = mx_units(d);
     hipLaunchKernelGGL(mx_rows_kernel<T>, dim3(l.blocks, (units + kRowWaves - 1) / kRowWaves), dim3(kRowThreads), 0, st, x, idx, perm, offsets, P, E, s.top_k, d,
                        starts, slot, ws + l.xq, ws + l.xq + (size_t)l.blocks * units * kMxCodes);
-    const MxTiles tiles = mx_tiles(P, E, d, F);
-    auto product = [&](bool swiglu, int rows, const void* w0, const void* w1, char* a, char* out, int N, int K) {
+    auto product = [&](bool swiglu, const void* w0, const void* w1, char* a, char* out, int N, int K) {
+        const int rows = mx_tile_rows(swiglu, P, E, N, K);
         return rows <= 32 ? launch_mx_stream(swiglu, s.act_dtype, w0, w1, a, out, starts, P, E, l.blocks, N, K, st)
                           : launch_mx_gemm(swiglu, s.act_dtype, w0, w1, a, out, starts, P, E, l.blocks, N, K, rows, st);
     };
-    int rc = product(true, tiles.hidden, w.gate, w.up, ws + l.xq, ws + l.hq, F, d);
-    if (rc == MOE_OK) rc = product(false, tiles.down, w.down, nullptr, ws + l.hq, ws + l.y, d, F);
+    int rc = product(true, w.gate, w.up, ws + l.xq, ws + l.hq, F, d);
+    if (rc == MOE_OK) rc = product(false, w.down, nullptr, ws + l.hq, ws + l.y, d, F);
     if (rc != MOE_OK) return rc;
     const int pieces = d / Store<T>::VEC;
     const long long all = (long long)s.n_tokens * pieces;
