@@ -298,16 +298,17 @@ def make_route_config(score=SCORE_SOFTMAX, n_groups=1, groups_kept=1, group_top=
 
 def _want(name: str, t: torch.Tensor, dtype, *shape) -> torch.Tensor:
     """t, if it has this type and shape: the library takes pointers and cannot tell."""
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if tuple(t.shape) != shape:
+    if t.shape != shape:
         raise ValueError(f"{name} must have shape {list(shape)}, got {list(t.shape)}")
     return t
 
 
 def _same_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> None:
+    at = first.get_device()
     for t in others:
-        if t is not None and t.device != first.device:
+        if t is not None and t.get_device() != at:
             raise ValueError(f"tensors on {first.device} and {t.device}")
 
 

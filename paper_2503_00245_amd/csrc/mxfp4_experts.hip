@@ -98,12 +98,27 @@ __global__ __launch_bounds__(kThreads) void mx_combine_kernel(const T* __restric
         float f[S::VEC];
 #pragma unroll
         for (int q = 0; q < S::VEC; ++q) f[q] = 0.f;
-        for (int j = 0; j < k; ++j) {
-            const int r = min(max(slot[t * k + j], 0), last_row);  // (in range for picks of no expert as well)
-            const float g = gate[t * k + j];
-            const typename S::vec_t v = *reinterpret_cast<const typename S::vec_t*>(rows + r * d + at);
+        // (four rows at a time: one after the other, each waits for its place and then for itself)
+        for (int j0 = 0; j0 < k; j0 += 4) {
+            int r[4];
+            float w[4];
+            typename S::vec_t v[4];
 #pragma unroll
-            for (int q = 0; q < S::VEC; ++q) f[q] = fmaf(g, S::get(v, q), f[q]);
+            for (int j = 0; j < 4; ++j) {
+                r[j] = slot[t * k + min(j0 + j, k - 1)];
+                w[j] = gate[t * k + min(j0 + j, k - 1)];
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                r[j] = min(max(r[j], 0), last_row);  // (in range for picks of no expert as well)
+                if (j0 + j < k) v[j] = *reinterpret_cast<const typename S::vec_t*>(rows + r[j] * d + at);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (j0 + j >= k) break;
+#pragma unroll
+                for (int q = 0; q < S::VEC; ++q) f[q] = fmaf(w[j], S::get(v[j], q), f[q]);
+            }
         }
         if (residual) {
             const typename S::vec_t v = *reinterpret_cast<const typename S::vec_t*>(residual + t * d + at);
@@ -146,14 +161,14 @@ MxLayout mx_layout(const moe_shape& s) {
 
 // Rows of a tile of a product of P rows in E groups: 32 (mxfp4_stream.hip), 64, 128 or 256 (mxfp4_gemm.hip), whichever is the shortest by what
 // they measured, in us.  Tiles: rounds of 256 workgroups, a round so much a tile and so much a unit of K.  Streamed: so much of a CU for 32 rows of
-// weights by 32, or the weights at 4.6 TB/s (in tiles 3.5).  How unevenly the rows are spread the host does not know: half a tile more
+// weights by 32.  In no case less than the weights at 4.6 TB/s.  How unevenly the rows are spread the host does not know: half a tile more
 // an expert.  Whole layers, us, this choice / the best of eight pairs of choices: 2048 / 5632, 2 of 8 experts, 200 tokens 56.8 / 54.0, 400 63.8 / 63.8, 800
 // 75.5 / 75.5, 1200 94.1 / 89.6, 2048 132.2 / 132.2; 1024 / 2816, 256 tokens 24.2 / 23.9, 2048 55.2 / 55.2; 1440 / 3840, 777 tokens 51.9 / 51.9; 432 / 1152,
 // 300 tokens 15.9 / 15.9.
 static int mx_tile_rows(bool swiglu, int P, int E, int N, int K) {
     const double rows = (double)P / E, units = mx_units(K), weights_mb = 0.53e-6 * N * (double)K * (swiglu ? 2 : 1) * std::min(P, E);
     auto groups = [&](int of) { return std::min((double)P, E * std::max(1.0, rows / of + 0.5)); };
-    double best = std::max(mx_blocks(N) * groups(32) / 256 * (0.35 + units * (swiglu ? 0.10 : 0.08)), weights_mb / 4.6) + 3.0;
+    double best = std::max(mx_blocks(N) * groups(32) / 256 * (0.35 + units * (swiglu ? 0.11 : 0.09)), weights_mb / 4.6) + 3.0;
     int choice = 32;
     struct {
         int rows;
@@ -161,7 +176,7 @@ static int mx_tile_rows(bool swiglu, int P, int E, int N, int K) {
     } const tiles[] = {{64, swiglu ? 3.8 : 4.9, 0.55}, {128, 4.8, 0.85}, {256, swiglu ? 6.0 : 5.0, 1.52}};
     for (const auto& t : tiles) {
         const double rounds = std::ceil(groups(t.rows) * ((N + (swiglu ? 127 : 255)) / (swiglu ? 128 : 256)) / 256);
-        const double us = std::max(rounds * (t.tile + units * t.unit), weights_mb / 3.5) + 1.5;
+        const double us = std::max(rounds * (t.tile + units * t.unit), weights_mb / 4.6) + 1.5;
         if (us < best) best = us, choice = t.rows;
     }
     return choice;

@@ -63,7 +63,7 @@ __device__ __forceinline__ size_t row_scale(int p, int c, int q, int units) {
     return ((size_t)(p >> 5) * units + (c >> 1)) * kMxScales + (q * 16 + (p & 15)) * 4 + (c & 1) * 2 + (p >> 4 & 1);
 }
 
-constexpr int kHiddenWaves = 8;
+constexpr int kHiddenWaves = 4;  // (of 2048 / 5632, us, with eight: two tokens 19.7 -> 19.4, four 35.6 -> 34.0)
 
 template <typename T>
 __global__ __launch_bounds__(kHiddenWaves* kWave) void mx_few_hidden_kernel(ptr_arg a_idx, ptr_arg a_x, ptr_arg a_gate, ptr_arg a_up, int P, int E, int k, int d,
@@ -176,12 +176,21 @@ __global__ __launch_bounds__(kDownWaves* kWave) void mx_few_down_kernel(ptr_arg 
                                                                         int F, size_t h_scales, ptr_arg a_residual, ptr_arg a_y) {
     __shared__ f32x4 s_part[kDownWaves][kWave];  // [expert in use x part of K]
     __shared__ int s_place[kMxFewPairs];         // of a pair: the first item of its expert * 16 + its row
+    __shared__ float s_gate[kMxFewPairs];
     const char* const h = from_arg<const char>(a_h);
     const char* const w = from_arg<const char>(a_down);
     const float* const gate = from_arg<const float>(a_pick_gate);
+    const T* const residual = from_arg<const T>(a_residual);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int ln = lane & 15, q = lane >> 4;
     const int fb = blockIdx.x >> 1, tile = blockIdx.x & 1, fbs = mx_blocks(d), units = mx_units(F);
+    // Four neighbouring columns a thread: token t, columns 32 fb + 8 a + 4 tile ...  (What the end needs is requested at the start.)
+    typedef typename Four<T>::vec_t four_t;
+    const int t = threadIdx.x >> 2, a = threadIdx.x & 3, col = fb * 32 + a * 8 + tile * 4;
+    const bool mine = t * k < P && col < d;
+    four_t base{};
+    if (mine && residual) base = *reinterpret_cast<const four_t*>(residual + (size_t)t * d + col);
+    const float my_gate = wave == 0 && lane < P ? gate[lane] : 0.f;
     Picks picks;
     picks.load(from_arg<const int32_t>(a_idx), P, E, lane);
     const unsigned long long used = picks.used();
@@ -194,7 +203,7 @@ __global__ __launch_bounds__(kDownWaves* kWave) void mx_few_down_kernel(ptr_arg 
         const size_t at = ((size_t)e * fbs + fb) * units, scales = (size_t)E * fbs * units * kMxCodes;
         const int pair = max(picks.pair_of_row(e, ln), 0);
         f32x4 acc{0.f, 0.f, 0.f, 0.f};
-        constexpr int U = 4;
+        constexpr int U = 6;  // (5632 columns in eight parts: all of a wave's requests at once)
         for (int c0 = c_begin; c0 < c_end; c0 += U) {
             i32x4 wv[U], hv[U];
             int ws[U], hs[U];
@@ -219,13 +228,11 @@ __global__ __launch_bounds__(kDownWaves* kWave) void mx_few_down_kernel(ptr_arg 
         int row = 0;
 #pragma unroll
         for (int p = 0; p < kMxFewPairs; ++p) row += p < lane && MOE_READLANE(picks.key, p) == picks.key ? 1 : 0;
+        s_gate[lane] = my_gate;
         s_place[lane] = picks.key < 0 ? -1 : __popcll(used & ((1ull << picks.key) - 1)) * parts * 16 + row;
     }
     __syncthreads();
-    // Four neighbouring columns a thread: token t, columns 32 fb + 8 a + 4 tile ...
-    typedef typename Four<T>::vec_t four_t;
-    const int t = threadIdx.x >> 2, a = threadIdx.x & 3, col = fb * 32 + a * 8 + tile * 4;
-    if (t * k >= P || col >= d) return;
+    if (!mine) return;
     float f[4] = {0.f, 0.f, 0.f, 0.f};
     for (int j = 0; j < k; ++j) {
         const int place = s_place[t * k + j];
@@ -237,19 +244,13 @@ __global__ __launch_bounds__(kDownWaves* kWave) void mx_few_down_kernel(ptr_arg 
 #pragma unroll
             for (int c = 0; c < 4; ++c) sum[c] += o[c];
         }
-        const float g = gate[t * k + j];
+        const float g = s_gate[t * k + j];
 #pragma unroll
         for (int c = 0; c < 4; ++c) f[c] = fmaf(g, sum[c], f[c]);
     }
-    const T* const residual = from_arg<const T>(a_residual);
     four_t o;
-    if (residual) {
-        const four_t r = *reinterpret_cast<const four_t*>(residual + (size_t)t * d + col);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) f[c] += (float)r[c];
-    }
-#pragma unroll
-    for (int c = 0; c < 4; ++c) o[c] = Store<T>::from_f32(f[c]);
+    for (int c = 0; c < 4; ++c) o[c] = Store<T>::from_f32(f[c] + (float)base[c]);
     *reinterpret_cast<four_t*>(from_arg<T>(a_y) + (size_t)t * d + col) = o;
 }
 

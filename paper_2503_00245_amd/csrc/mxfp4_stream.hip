@@ -12,7 +12,8 @@ namespace {
 
 constexpr int kWaves = 4;
 
-template <bool SWIGLU, typename T>
+// ONCE: most experts have one group of rows, and the weights need not stay in the caches (2048 / 5632, 32 tokens 46.1 -> 43.7 us a layer)
+template <bool SWIGLU, bool ONCE, typename T>
 __global__ __launch_bounds__(kWaves* kWave) void mx_stream_kernel(ptr_arg a_starts, ptr_arg a_w0, ptr_arg a_w1, ptr_arg a_rows, int E, int N, int K, int all_blocks,
                                                                   ptr_arg a_out) {
     constexpr int M = SWIGLU ? 2 : 1, NT = 2;  // matrices, tiles of 16 rows
@@ -41,7 +42,10 @@ __global__ __launch_bounds__(kWaves* kWave) void mx_stream_kernel(ptr_arg a_star
 #pragma unroll
         for (int m = 0; m < M; ++m) {
 #pragma unroll
-            for (int ct = 0; ct < 4; ++ct) fa[m][ct / 2][ct % 2] = *reinterpret_cast<const i32x4*>(w_of[m] + (at + u) * kMxCodes + ct * 1024 + lane * 16);
+            for (int ct = 0; ct < 4; ++ct) {
+                const i32x4* p = reinterpret_cast<const i32x4*>(w_of[m] + (at + u) * kMxCodes + ct * 1024 + lane * 16);
+                fa[m][ct / 2][ct % 2] = ONCE ? __builtin_nontemporal_load(p) : *p;
+            }
             sa[m] = *reinterpret_cast<const int*>(w_of[m] + scales + (at + u) * kMxScales + lane * 4);
         }
         const size_t row_at = (size_t)sb * units + u;
@@ -86,8 +90,12 @@ int launch_mx_stream(bool swiglu, int act_dtype, const void* w0, const void* w1,
         hipLaunchKernelGGL(kern, grid, dim3(kWaves * kWave), 0, st, as_arg(starts), as_arg(w0), as_arg(w1), as_arg(a), E, N, K, all_blocks, as_arg(out));
         return launch_status();
     };
-    if (swiglu) return launch(mx_stream_kernel<true, bf16_t>);  // (its output is codes, whatever the type)
-    return act_dtype == MOE_F32 ? launch(mx_stream_kernel<false, float>) : launch(mx_stream_kernel<false, bf16_t>);
+    auto launch_type = [&](auto once) {
+        constexpr bool O = decltype(once)::value;
+        if (swiglu) return launch(mx_stream_kernel<true, O, bf16_t>);  // (its output is codes, whatever the type)
+        return act_dtype == MOE_F32 ? launch(mx_stream_kernel<false, O, float>) : launch(mx_stream_kernel<false, O, bf16_t>);
+    };
+    return P <= 32 * E ? launch_type(std::true_type{}) : launch_type(std::false_type{});
 }
 
 }  // namespace moe
