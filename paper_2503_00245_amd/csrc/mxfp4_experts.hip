@@ -55,34 +55,33 @@ __global__ __launch_bounds__(kRowThreads) void mx_rows_kernel(const T* __restric
         __syncthreads();
     }
     if (blockIdx.y == 0 && threadIdx.x < n) slot[s_pair[threadIdx.x]] = block * 32 + threadIdx.x;
-    const int u = blockIdx.y * kRowWaves + wave;
+    // a wave takes a k-step of 128 columns
+    const int step = blockIdx.y * kRowWaves + wave, u = step >> 1, c = step & 1;
     if (u >= units) return;
-    const int q = lane >> 4;
+    const int col = step * 128 + (lane >> 4) * 32;
     unsigned scale = 0;
-    typename S::vec_t v[4][VECS];
+    typename S::vec_t v[2][VECS];
 #pragma unroll
-    for (int ct = 0; ct < 4; ++ct) {
-        const int p = s_pair[min(16 * (ct & 1) + (lane & 15), n - 1)];  // (rows past the last are the last one again)
+    for (int t = 0; t < 2; ++t) {
+        const int p = s_pair[min(16 * t + (lane & 15), n - 1)];  // (rows past the last are the last one again)
         const T* row = x + (size_t)quick_div(p, k) * d;
-        const int col = u * kMxUnit + (ct >> 1) * 128 + q * 32;
 #pragma unroll
-        for (int i = 0; i < VECS; ++i) v[ct][i] = *reinterpret_cast<const typename S::vec_t*>(row + min(col + i * S::VEC, d - S::VEC));
+        for (int i = 0; i < VECS; ++i) v[t][i] = *reinterpret_cast<const typename S::vec_t*>(row + min(col + i * S::VEC, d - S::VEC));
     }
 #pragma unroll
-    for (int ct = 0; ct < 4; ++ct) {
-        const int col = u * kMxUnit + (ct >> 1) * 128 + q * 32;
+    for (int t = 0; t < 2; ++t) {
         if (col + 32 > d) {
 #pragma unroll
             for (int i = 0; i < VECS; ++i)
-                if (col + i * S::VEC >= d) v[ct][i] = typename S::vec_t{};
+                if (col + i * S::VEC >= d) v[t][i] = typename S::vec_t{};
         }
-        i32x4 c;
+        i32x4 codes8;
         int b;
-        mx_quantise_32<T>(v[ct], c, b);
-        *reinterpret_cast<i32x4*>(codes + ((size_t)block * units + u) * kMxCodes + ct * 1024 + lane * 16) = c;
-        scale |= (unsigned)b << (8 * ct);
+        mx_quantise_32<T>(v[t], codes8, b);
+        *reinterpret_cast<i32x4*>(codes + ((size_t)block * units + u) * kMxCodes + (c * 2 + t) * 1024 + lane * 16) = codes8;
+        scale |= (unsigned)b << (8 * t);
     }
-    *reinterpret_cast<unsigned*>(scales + ((size_t)block * units + u) * kMxScales + lane * 4) = scale;
+    *reinterpret_cast<uint16_t*>(scales + ((size_t)block * units + u) * kMxScales + lane * 4 + c * 2) = (uint16_t)scale;
 }
 
 // ---- combine --------------------------------------------------------------------------------------------------------
@@ -197,7 +196,7 @@ static int experts(const moe_shape& s, const moe_mxfp4_weights& w, const T* x, c
         offsets = reinterpret_cast<int32_t*>(ws + l.offsets);
     }
     const int units = mx_units(d);
-    hipLaunchKernelGGL(mx_rows_kernel<T>, dim3(l.blocks, (units + kRowWaves - 1) / kRowWaves), dim3(kRowThreads), 0, st, x, idx, perm, offsets, P, E, s.top_k, d,
+    hipLaunchKernelGGL(mx_rows_kernel<T>, dim3(l.blocks, (2 * units + kRowWaves - 1) / kRowWaves), dim3(kRowThreads), 0, st, x, idx, perm, offsets, P, E, s.top_k, d,
                        starts, slot, ws + l.xq, ws + l.xq + (size_t)l.blocks * units * kMxCodes);
     auto product = [&](bool swiglu, const void* w0, const void* w1, char* a, char* out, int N, int K) {
         const int rows = mx_tile_rows(swiglu, P, E, N, K);
