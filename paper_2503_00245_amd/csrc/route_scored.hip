@@ -210,7 +210,7 @@ __device__ __forceinline__ void route_exactly(const RouteArgs& g, int t, double*
 
 // ---- a token to a row of 16 lanes --------------------------------------------------------------------------------
 // Exchanges inside a row are register operations (DPP), and a wave has four tokens: the wave-wide form above, for every token, took
-// 59 us at 16384 tokens of 256 experts where this takes 15.
+// 59 us at 16384 tokens of 256 experts where this takes 16, and 22 with some tokens on the long way.
 constexpr int kTeam = 16;
 constexpr int kNowhere = 1 << 20;  // above every index
 template <typename F, typename Op>
@@ -495,78 +495,121 @@ __global__ __launch_bounds__(kWaves* kWave) void route_scored_kernel(const Route
     }
 }
 
-template <int V>
+// ---- the gradient ------------------------------------------------------------------------------------------------------
+// Of the gates g_j = scale w_j / sum w, w the picked scores, the derivative of a loss with gradient dg is, for the logit of pick j,
+//   g_j (dg_j - sum_i dg_i g_i / scale), with a sigmoid times 1 - s_j:
+// the softmax's own coupling adds nothing, since sum_j w_j d(loss)/d(w_j) = 0.  In this form no score is divided by, so
+// that rows of tiny scores keep their gradient.  Without renormalisation, and for gradients of the scores themselves,
+// d(loss)/d(l_e) = s_e (ds_e - sum ds s), or ds_e s_e (1 - s_e).
+// A wave takes a token; four neighbouring experts to a lane where rows allow it (FOUR).  Bound by memory.  (16384 tokens of 256 experts,
+// without a gradient of the
+// scores, us: 13.9 with all scores formed, 9.5 now; a copy of as many bytes 7.)
+template <int V, bool FOUR>
 __global__ __launch_bounds__(kWaves* kWave) void route_scored_backward_kernel(const float* __restrict__ logits, const int32_t* __restrict__ topk_idx,
                                                                               const float* __restrict__ grad_gate, const float* __restrict__ grad_scores,
                                                                               float* __restrict__ grad_logits, int T, int E, int k, int sigmoid,
                                                                               int renormalize, float scale) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int t = blockIdx.x * kWaves + wave;
-    __shared__ float s_ds[kWaves][V * kWave];
-    if (t >= T) return;
+    __shared__ __align__(16) float s_add[kWaves][V * kWave];
+    if (t >= T) return;  // (waves exchange nothing)
     const float* row = logits + (size_t)t * E;
-    float l[V], ds[V];
-    float top = -INFINITY;
+    constexpr int W = FOUR ? 4 : 1;  // neighbours of a lane
+    static_assert(V % W == 0, "whole pieces");
+    typedef float piece_t __attribute__((ext_vector_type(W)));
+    auto expert = [&](int v) { return (v / W * kWave + lane) * W; };  // the first of piece v / W
+    auto load = [&](const float* from, float (&out)[V], float beyond) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const int e = v * kWave + lane;
-        l[v] = e < E ? row[e] : -INFINITY;
-        ds[v] = e < E && grad_scores ? grad_scores[(size_t)t * E + e] : 0.f;
-        if (!(l[v] == l[v])) l[v] = -INFINITY;
-        top = fmaxf(top, l[v]);
-        s_ds[wave][v * kWave + lane] = 0.f;
-    }
+        for (int v = 0; v < V; v += W) {
+            const piece_t p = *reinterpret_cast<const piece_t*>(from + min(expert(v), E - W));
+#pragma unroll
+            for (int i = 0; i < W; ++i) out[v + i] = expert(v) < E ? p[i] : beyond;
+        }
+    };
     const int e_of = lane < k ? topk_idx[(size_t)t * k + lane] : -1;
-    const bool named = lane < k && (unsigned)e_of < (unsigned)E;
+    const bool named = (unsigned)e_of < (unsigned)E;
     const float dg = named ? grad_gate[(size_t)t * k + lane] : 0.f;
     float pl = named ? row[e_of] : -INFINITY;
     if (!(pl == pl)) pl = -INFINITY;
-    float s[V], den = 0.f;
-    const float base = sigmoid ? 0.f : wave_max(top) == -INFINITY ? 0.f : wave_max(top);
+    // Without a gradient of the scores the logits that were not picked have none, and are not read, unless a softmax's sum couples them
+    const bool all = grad_scores || !(renormalize || sigmoid);
+    float l[V], ds[V], s[V], base = 0.f, den = 1.f;
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        s[v] = sigmoid ? 1.f / (1.f + expf(-l[v])) : expf(l[v] - base);
-        den += s[v];
-    }
-    den = wave_sum(den);
-    if (!sigmoid) {
+    for (int v = 0; v < V; ++v) l[v] = -INFINITY, ds[v] = s[v] = 0.f;
+    if (all) {
+        load(row, l, -INFINITY);
+        if (grad_scores) load(grad_scores + (size_t)t * E, ds, 0.f);
+        float top = -INFINITY;
 #pragma unroll
-        for (int v = 0; v < V; ++v) s[v] = den > 0.f ? s[v] / den : 0.f;
+        for (int v = 0; v < V; ++v) {
+            if (!(l[v] == l[v])) l[v] = -INFINITY;
+            top = fmaxf(top, l[v]);
+        }
+        if (sigmoid) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) s[v] = quick_sigmoid(l[v]);
+        } else {
+            top = wave_max(top);
+            base = top == -INFINITY ? 0.f : top;
+            den = 0.f;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                s[v] = __expf(l[v] - base);
+                den += s[v];
+            }
+            den = wave_sum(den);
+            const float inv = den > 0.f ? 1.f / den : 0.f;
+#pragma unroll
+            for (int v = 0; v < V; ++v) s[v] *= inv;
+        }
     }
-    // d(loss)/d(logit) of the gates, but for the part that all logits of a softmax share
+#pragma unroll
+    for (int v = 0; v < V; v += W) *reinterpret_cast<piece_t*>(&s_add[wave][expert(v)]) = piece_t(0.f);
+    // what a pick adds to the gradient of its logit
     float add;
+    const float slope = sigmoid ? 1.f / (1.f + expf(pl)) : 1.f;  // 1 - s
     if (renormalize) {
         const float big = wave_max(pl);
-        const float m = big == -INFINITY ? 0.f : sigmoid ? fminf(big, 0.f) : big;
         float w = 0.f;
-        if (pl != -INFINITY) w = !sigmoid ? expf(pl - m) : pl >= 0.f ? 1.f / (1.f + expf(-pl)) : expf(pl - m) / (1.f + expf(pl));
+        if (pl != -INFINITY) w = pick_weight(pl, sigmoid ? fminf(big, 0.f) : big, sigmoid);
         const float total = wave_sum(w);
         const float g = total > 0.f ? w / total : 0.f;
-        const float mean = wave_sum(dg * g);
-        add = scale * g * (dg - mean) * (sigmoid ? 1.f / (1.f + expf(pl)) : 1.f);
+        add = scale * g * (dg - wave_sum(dg * g)) * slope;
     } else {
-        const float sp = sigmoid ? 1.f / (1.f + expf(-pl)) : den > 0.f ? expf(pl - base) / den : 0.f;
-        add = scale * dg * sp * (sigmoid ? 1.f / (1.f + expf(pl)) : 1.f);
+        add = scale * dg * (sigmoid ? 1.f / (1.f + expf(-pl)) : den > 0.f ? expf(pl - base) / den : 0.f) * slope;
+    }
+    // an expert may be named twice: then one pick after the other, so that sums have an order
+    bool again = false;
+    for (int j = 1; j < k; ++j) {
+        const int o = MOE_READLANE(e_of, j);
+        again |= named && lane < j && o == e_of;
     }
     wave_lds();
-    for (int j = 0; j < k; ++j) {  // (one after the other: an expert may be named twice)
-        if (lane == j && named) s_ds[wave][e_of] += add;
-        wave_lds();
+    if (!__ballot(again)) {
+        if (named) s_add[wave][e_of] = add;
+    } else {
+        for (int j = 0; j < k; ++j) {
+            if (lane == j && named) s_add[wave][e_of] += add;
+            wave_lds();
+        }
     }
+    wave_lds();
     float shared = 0.f;
-    if (!sigmoid) {
+    if (!sigmoid && all) {
         float part = renormalize || !named ? 0.f : add;
 #pragma unroll
         for (int v = 0; v < V; ++v) part += ds[v] * s[v];
         shared = wave_sum(part);
     }
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const int e = v * kWave + lane;
-        if (e < E) {
-            const float own = sigmoid ? ds[v] * s[v] * (l[v] == -INFINITY ? 0.f : 1.f / (1.f + expf(l[v]))) : s[v] * (ds[v] - shared);
-            grad_logits[(size_t)t * E + e] = s_ds[wave][e] + own;
-        }
+    for (int v = 0; v < V; v += W) {
+        const int e = expert(v);
+        if (e >= E) continue;
+        piece_t o = *reinterpret_cast<const piece_t*>(&s_add[wave][e]);
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+            o[i] += sigmoid ? ds[v + i] * s[v + i] * quick_sigmoid(-l[v + i]) : s[v + i] * (ds[v + i] - shared);
+        *reinterpret_cast<piece_t*>(grad_logits + (size_t)t * E + e) = o;
     }
 }
 
@@ -677,9 +720,17 @@ extern "C" int moe_route_scored_backward(const moe_route_config* config, int32_t
         !aligned4(grad_scores) || !aligned4(grad_logits) || grad_logits == logits || grad_logits == grad_scores)
         return MOE_ERR_INVALID;
     const moe_route_config& c = *config;
+    // four experts to a lane: rows of whole 16-byte pieces
+    const bool four = n_experts >= 256 && n_experts % 4 == 0 && aligned16(logits) && aligned16(grad_scores) && aligned16(grad_logits);
     return with_values(n_experts, [&](auto V) {
-        hipLaunchKernelGGL(route_scored_backward_kernel<V.value>, dim3((n_tokens + kWaves - 1) / kWaves), dim3(kWaves * kWave), 0, as_stream(stream),
-                           logits, topk_idx, grad_gate, grad_scores, grad_logits, n_tokens, n_experts, top_k, c.score, c.renormalize, c.scale);
-        return launch_status();
+        constexpr int v = decltype(V)::value;
+        auto launch = [&](auto kern) {
+            hipLaunchKernelGGL(kern, dim3((n_tokens + kWaves - 1) / kWaves), dim3(kWaves * kWave), 0, as_stream(stream), logits, topk_idx, grad_gate,
+                               grad_scores, grad_logits, n_tokens, n_experts, top_k, c.score, c.renormalize, c.scale);
+            return launch_status();
+        };
+        if constexpr (v >= 4)
+            if (four) return launch(route_scored_backward_kernel<v, true>);
+        return launch(route_scored_backward_kernel<v, false>);
     });
 }
