@@ -168,6 +168,7 @@ static int mx_tile_rows(bool swiglu, int P, int E, int N, int K) {
     const double rows = (double)P / E, units = mx_units(K), weights_mb = 0.53e-6 * N * (double)K * (swiglu ? 2 : 1) * std::min(P, E);
     auto groups = [&](int of) { return std::min((double)P, E * std::max(1.0, rows / of + 0.5)); };
     double best = std::max(mx_blocks(N) * groups(32) / 256 * (0.35 + units * (swiglu ? 0.11 : 0.09)), weights_mb / 4.6) + 3.0;
+    if (groups(32) + E > 65535) best = 1e30;  // (more than the grid's second dimension has)
     int choice = 32;
     struct {
         int rows;
@@ -220,10 +221,13 @@ int launch_mx_experts(const moe_shape& s, const moe_mxfp4_weights& w, const void
     return experts<bf16_t>(s, w, static_cast<const bf16_t*>(x), idx, gate, static_cast<bf16_t*>(y), l, ws, st);
 }
 
+constexpr int kMxMaxWidth = 1 << 18;
 static int validate_mx(const moe_shape* s) {
     const int rc = validate_shape(s);
     if (rc != MOE_OK) return rc;
     if (s->flags & MOE_FLAG_SHARED_BASE) return MOE_ERR_INVALID;
+    // (tiles are counted, and scales of a matrix found, in 32 bits)
+    if (s->d_model > kMxMaxWidth || s->d_ff > kMxMaxWidth) return MOE_ERR_UNSUPPORTED;
     return s->rank ? MOE_ERR_UNSUPPORTED : MOE_OK;
 }
 static int validate_call(const moe_shape* s, const moe_mxfp4_weights* w, const void* x, const void* y) {

@@ -10,6 +10,13 @@
 //
 // The eight waves are two groups, one wave of each on every SIMD, half a unit apart: while one multiplies out of
 // registers, the other reads the fragments of its next unit.  Group 1 fetches, between its products.
+// Measured on 2048 / 5632, Zipf loads, us (products of a wave for itself straight from memory / this): gate/up 105 / 72 and down 69 / 38 at 2048 tokens,
+// 699 / 440 and 500 / 205 at 16384 (3.5 PFLOP/s; a loop of these instructions on random operands and nothing else 7.1, the clock at 1.7 GHz
+// under the board's power limit).  The matrix units are busy 42 % of the clocks, at 2.05 GHz; a tile of 256 by 256 takes 3200 clocks a unit and 14000
+// beside them, of which 7000 are the activation's exponentials and reciprocals.
+// Measured and not adopted: tiles one after the other in a workgroup, the fills running on into the next (477 and 207); fills by the
+// group that reads (486 and 237: they stand before the reads); four waves of 128 by 128 and 256 accumulators, two thirds of the fragment reads
+// but one wave to a SIMD (607 and 251); fills every second product, column tiles in blocks of one, two or eight: none.
 #include <algorithm>
 
 #include "gemm.h"
@@ -23,6 +30,7 @@ namespace {
 #define INLINE __attribute__((always_inline))
 
 constexpr int kThreads = 512;
+constexpr int kSplitSlots = 32;  // one workgroup per CU
 
 struct MxGemmArgs {
     const char *w0, *w1;  // packed weights (w1: up, with SWIGLU)
@@ -59,7 +67,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         hi = g.starts[lane + 1] * 32;
     }
     auto n_tiles_of = [&](int) INLINE { return (out_blocks + OUT_BLOCKS - 1) / OUT_BLOCKS; };
-    if (!find_tile<4>(lo, hi, g.E, BS, n_tiles_of, e, row0, row_end, nt)) return;
+    // (blocks of four column tiles, and the tiles of a last round that is half full at most in two: 16384 tokens of 2048 / 5632, down 209 -> 203 us)
+    if (!find_tile<4, kSplitSlots>(lo, hi, g.E, BS, n_tiles_of, e, row0, row_end, nt)) return;
     const int sb0 = row0 >> 5, live_blocks = min(SBLK, (row_end - row0) >> 5);
     const int fb0 = nt * OUT_BLOCKS;
     const int grp = wave >> 2, wm = (wave % (2 * WM)) % WM, ws = wave / WM;
@@ -245,7 +254,7 @@ int launch_tile(const MxGemmArgs& g, int P, hipStream_t st) {
     auto kern = mx_gemm_kernel<BS, NST, SWIGLU, T>;
     static std::atomic<uint64_t> allowed{0};
     if (allow_dynamic_lds(reinterpret_cast<const void*>(kern), lds, allowed) != MOE_OK) return MOE_ERR_LAUNCH;
-    hipLaunchKernelGGL(kern, dim3(find_tile_grid(tiles, 0)), dim3(kThreads), lds, st, g);
+    hipLaunchKernelGGL(kern, dim3(find_tile_grid(tiles, kSplitSlots)), dim3(kThreads), lds, st, g);
     return launch_status();
 }
 

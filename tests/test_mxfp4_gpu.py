@@ -124,6 +124,7 @@ SHAPES = [  # T, d, F, E, k, skew
     (3, 40, 72, 3, 3, 0), (5, 400, 1064, 8, 2, 1), (16, 512, 776, 4, 4, 0), (17, 264, 304, 5, 2, 0), (32, 136, 520, 64, 8, 0), (32, 264, 72, 3, 2, 0), (24, 1024, 512, 16, 4, 0),
     (33, 128, 256, 2, 1, 3), (40, 256, 2048, 8, 2, 1), (64, 640, 1728, 4, 1, 9), (100, 72, 40, 64, 6, 0), (130, 432, 1152, 8, 2, 1),
     (257, 520, 328, 4, 2, 2), (300, 256, 256, 1, 1, 0), (513, 200, 456, 8, 3, 1), (1100, 136, 264, 8, 8, 0), (5000, 64, 96, 32, 2, 1),
+    (20000, 8, 16, 1, 1, 0), (9000, 40, 72, 64, 1, 2),
 ]
 
 
@@ -256,3 +257,29 @@ def test_an_expert_that_a_token_names_twice_counts_twice(T, E, k):
     y = _run(x, w, torch.from_numpy(idx).to(dev()), torch.from_numpy(gate).to(dev()), E, k, d, F, "bf16", False)
     ref, tol = oo.experts(x.double().cpu().numpy(), exact, idx, gate.astype(np.float64), False, 2.0 ** -8)
     assert (np.abs(y.double().cpu().numpy() - ref) <= tol).all()
+
+
+def test_the_example_runs():
+    # rounding to E2M1 under a scale for 32 normal values is off by about 0.115 of the norm (0.13 where a block's largest magnitude is above
+    # 6 scales); inputs, two products' weights and the hidden row add up in squares: 0.115 sqrt(2) after the first product, on either branch of the
+    # SwiGLU, then a rounding more on both sides: between 0.2 and 0.35
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "quantised_layer.py")
+    spec = importlib.util.spec_from_file_location("quantised_layer", path)
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    errors = mod.main(tokens=70, experts=16, d=256, f=512, top_k=2)
+    assert all(0.15 < e < 0.4 for e in errors), errors
+
+
+def test_more_groups_of_rows_than_a_grid_has_in_its_second_dimension():
+    T, d, F = 65536 * 32 + 40, 8, 8
+    rng = np.random.default_rng(1)
+    w, exact = _layer(rng, 1, d, F)
+    x = torch.randn(T, d, device=dev()).bfloat16()
+    idx, gate = torch.zeros(T, 1, dtype=torch.int32, device=dev()), torch.ones(T, 1, device=dev())
+    y = _run(x, w, idx, gate, 1, 1, d, F, "bf16", False)
+    for part in (slice(0, 50), slice(T // 2, T // 2 + 50), slice(T - 50, T)):
+        ref, tol = oo.experts(x[part].double().cpu().numpy(), exact, np.zeros((50, 1), np.int32), np.ones((50, 1)), False, 2.0 ** -8)
+        assert (np.abs(y[part].double().cpu().numpy() - ref) <= tol).all()

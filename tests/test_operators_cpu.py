@@ -117,7 +117,8 @@ def test_experts_refuse():
         assert call(w=_weights(down=4100)) == INVALID
         for bad, status in ((pkg.make_shape(8, 252, 512, 4, 2), UNSUPPORTED), (pkg.make_shape(8, 256, 512, 65, 2), UNSUPPORTED),
                             (pkg.make_shape(8, 256, 512, 4, 5), INVALID), (pkg.make_shape(8, 256, 512, 4, 2, rank=64), UNSUPPORTED),
-                            (pkg.make_shape(8, 256, 512, 4, 2, rank=64, flags=1), INVALID), (pkg.make_shape(8, 256, 512, 4, 2, act_dtype=3), UNSUPPORTED)):
+                            (pkg.make_shape(8, 256, 512, 4, 2, rank=64, flags=1), INVALID), (pkg.make_shape(8, 256, 512, 4, 2, act_dtype=3), UNSUPPORTED),
+                            (pkg.make_shape(8, 256, (1 << 18) + 8, 4, 2), UNSUPPORTED), (pkg.make_shape(8, (1 << 18) + 8, 512, 4, 2), UNSUPPORTED)):
             assert call(shape=bad) == status
             assert pkg.moe_mxfp4_workspace_bytes(bad) == 0
     assert experts(idx=None) == INVALID
