@@ -87,13 +87,23 @@ __device__ __forceinline__ unsigned mx_abs_max(const float (&v)[8]) {
     return m;
 }
 
+// Largest of the four lanes l, l ^ 16, l ^ 32, l ^ 48 (m >= 0), in all of them: rows of 16 lanes, then halves, change places between two
+// registers, so that nothing goes through LDS
+__device__ __forceinline__ int mx_max_of_rows(int m) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    const auto rows = __builtin_amdgcn_permlane16_swap(m, m, false, false);
+    m = max((int)rows[0], (int)rows[1]);
+    const auto halves = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+    return max((int)halves[0], (int)halves[1]);
+#else
+    return m;
+#endif
+}
+
 // Eight hidden columns (columns 32 fb + 8 (lane / 16) ..., row lane % 16 of tile n of block sb), quantised, into a matrix of `units`
 // units a block: a dword of codes a lane, and a byte of scale for four lanes.
 __device__ __forceinline__ void mx_store_hidden(const float (&f)[8], char* __restrict__ codes, char* __restrict__ scales, int units, int sb, int n, int fb, int lane) {
-    int m = (int)mx_abs_max(f);
-    m = max(m, __shfl_xor(m, 16, kWave));
-    m = max(m, __shfl_xor(m, 32, kWave));
-    const int b = mx_scale_byte(m), c = fb >> 2, at = (fb & 3) * 16 + (lane & 15);
+    const int b = mx_scale_byte(mx_max_of_rows((int)mx_abs_max(f))), c = fb >> 2, at = (fb & 3) * 16 + (lane & 15);
     const size_t unit = (size_t)sb * units + (c >> 1);
     *reinterpret_cast<unsigned*>(codes + unit * kMxCodes + ((c & 1) * 2 + n) * 1024 + at * 16 + (lane >> 4) * 4) = mx_codes8(f, b);
     if (lane < 16) scales[unit * kMxScales + at * 4 + (c & 1) * 2 + n] = (char)b;

@@ -176,7 +176,7 @@ static int mx_tile_rows(bool swiglu, int P, int E, int N, int K) {
     } const tiles[] = {{64, swiglu ? 3.8 : 4.9, 0.55}, {128, 4.8, 0.85}, {256, swiglu ? 6.0 : 5.0, 1.52}};
     for (const auto& t : tiles) {
         const double rounds = std::ceil(groups(t.rows) * ((N + (swiglu ? 127 : 255)) / (swiglu ? 128 : 256)) / 256);
-        const double us = std::max(rounds * (t.tile + units * t.unit), weights_mb / 4.6) + 1.5;
+        const double us = std::max(rounds * (t.tile + units * t.unit), weights_mb / 4.6) + 2.5;
         if (us < best) best = us, choice = t.rows;
     }
     return choice;

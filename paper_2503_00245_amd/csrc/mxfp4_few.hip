@@ -151,10 +151,7 @@ __global__ __launch_bounds__(kHiddenWaves* kWave) void mx_few_hidden_kernel(ptr_
 #pragma unroll
             for (int i = 0; i < 4; ++i) f[t * 4 + i] = silu_f32(g[i]) * u[i];
         }
-        int m = (int)mx_abs_max(f);
-        m = max(m, __shfl_xor(m, 16, kWave));
-        m = max(m, __shfl_xor(m, 32, kWave));
-        const int b = mx_scale_byte(m);
+        const int b = mx_scale_byte(mx_max_of_rows((int)mx_abs_max(f)));
         if (pair >= 0) {
             *reinterpret_cast<unsigned*>(out + row_codes(pair, fb >> 2, fb & 3, out_units) + q * 4) = mx_codes8(f, b);
             if (q == 0) out[out_scales + row_scale(pair, fb >> 2, fb & 3, out_units)] = (char)b;

@@ -14,7 +14,7 @@
 // 699 / 440 and 500 / 205 at 16384 (3.5 PFLOP/s; a loop of these instructions on random operands and nothing else 7.1, the clock at 1.7 GHz
 // under the board's power limit).  The matrix units are busy 42 % of the clocks, at 2.05 GHz; a tile of 256 by 256 takes 3200 clocks a unit and 14000
 // beside them, of which 7000 are the activation's exponentials and reciprocals.
-// Measured and not adopted: tiles one after the other in a workgroup, the fills running on into the next (477 and 207); fills by the
+// Measured and not adopted: tiles one after the other in a workgroup, the fills running on into the next (447 and 204, 477 with a wait behind the stores); fills by the
 // group that reads (486 and 237: they stand before the reads); four waves of 128 by 128 and 256 accumulators, two thirds of the fragment reads
 // but one wave to a SIMD (607 and 251); fills every second product, column tiles in blocks of one, two or eight: none.
 #include <algorithm>
