@@ -1,6 +1,5 @@
 // Routing from logits: scores by softmax or sigmoid, picks by score and bias inside the best groups, gates; and
-// the gradient of gates and scores with regard to the logits.  moe.h states the definition.
-//
+// the gradient of gates and scores with regard to the logits.  moe_quantised.h states the definition.
 #include <cmath>
 
 #include "mxfp4.h"
