@@ -312,61 +312,67 @@ def _same_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> None:
             raise ValueError(f"tensors on {first.device} and {t.device}")
 
 
+def _arg(name: str, t: Optional[torch.Tensor], dtype, shape, device: int):
+    """Pointer of a tensor that has this type, shape and device and is contiguous.  (All in one place: of calls that take
+    less time on the GPU than on the host, the checks of five tensors are most.)"""
+    if t is None:
+        return None
+    if t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous():
+        return t.data_ptr()
+    _want(name, t, dtype, *shape)
+    if t.get_device() != device:
+        raise ValueError(f"{name} on another device than the call's first tensor")
+    return _ptr(t)
+
+
 def moe_route_scored(config: RouteConfig, logits, select_bias, topk_idx, topk_gate, scores=None) -> None:
     """logits f32 [T,E], select_bias f32 [E] or None; topk_idx int32 [T,k], topk_gate f32 [T,k] and scores f32 [T,E]
     (or None): outputs."""
-    T, E = logits.shape
+    rows, at, f32 = logits.shape, logits.get_device(), torch.float32
+    T, E = rows
     k = topk_idx.shape[-1]
-    _want("logits", logits, torch.float32, T, E)
-    _want("topk_idx", topk_idx, torch.int32, T, k)
-    _want("topk_gate", topk_gate, torch.float32, T, k)
-    if select_bias is not None:
-        _want("select_bias", select_bias, torch.float32, E)
-    if scores is not None:
-        _want("scores", scores, torch.float32, T, E)
-    _same_device(logits, select_bias, topk_idx, topk_gate, scores)
-    _check("moe_route_scored", lib().moe_route_scored(
-        C.byref(config), T, E, k, _ptr(logits), _ptr(select_bias), _ptr(topk_idx), _ptr(topk_gate), _ptr(scores),
-        _stream(logits.device)))
+    picks = (T, k)
+    status = lib().moe_route_scored(
+        C.byref(config), T, E, k, _arg("logits", logits, f32, rows, at), _arg("select_bias", select_bias, f32, (E,), at),
+        _arg("topk_idx", topk_idx, torch.int32, picks, at), _arg("topk_gate", topk_gate, f32, picks, at),
+        _arg("scores", scores, f32, rows, at), _stream(logits.device))
+    if status:
+        raise MoeError("moe_route_scored", status)
 
 
 def moe_route_scored_backward(config: RouteConfig, logits, topk_idx, grad_gate, grad_scores, grad_logits) -> None:
     """logits f32 [T,E], topk_idx int32 [T,k] of the forward call, grad_gate f32 [T,k], grad_scores f32 [T,E] or None;
     grad_logits f32 [T,E]: output."""
-    T, E = logits.shape
+    rows, at, f32 = logits.shape, logits.get_device(), torch.float32
+    T, E = rows
     k = topk_idx.shape[-1]
-    _want("logits", logits, torch.float32, T, E)
-    _want("topk_idx", topk_idx, torch.int32, T, k)
-    _want("grad_gate", grad_gate, torch.float32, T, k)
-    if grad_scores is not None:
-        _want("grad_scores", grad_scores, torch.float32, T, E)
-    _want("grad_logits", grad_logits, torch.float32, T, E)
-    _same_device(logits, topk_idx, grad_gate, grad_scores, grad_logits)
-    _check("moe_route_scored_backward", lib().moe_route_scored_backward(
-        C.byref(config), T, E, k, _ptr(logits), _ptr(topk_idx), _ptr(grad_gate), _ptr(grad_scores), _ptr(grad_logits),
-        _stream(logits.device)))
+    picks = (T, k)
+    status = lib().moe_route_scored_backward(
+        C.byref(config), T, E, k, _arg("logits", logits, f32, rows, at), _arg("topk_idx", topk_idx, torch.int32, picks, at),
+        _arg("grad_gate", grad_gate, f32, picks, at), _arg("grad_scores", grad_scores, f32, rows, at),
+        _arg("grad_logits", grad_logits, f32, rows, at), _stream(logits.device))
+    if status:
+        raise MoeError("moe_route_scored_backward", status)
 
 
 def _mxfp4_rows(x, codes, scales):
-    cols = x.shape[-1]
-    _want("codes", codes, torch.uint8, *x.shape[:-1], cols // 2)
-    _want("scales", scales, torch.uint8, *x.shape[:-1], (cols + 31) // 32)
-    _same_device(x, codes, scales)
-    return x.numel() // max(cols, 1), cols
+    """(rows, columns, pointers of x, codes and scales)"""
+    shape, at = x.shape, x.get_device()
+    cols, lead = shape[-1], shape[:-1]
+    return (lead.numel(), cols, _ptr(x), _arg("codes", codes, torch.uint8, (*lead, cols // 2), at),
+            _arg("scales", scales, torch.uint8, (*lead, (cols + 31) // 32), at))
 
 
 def moe_mxfp4_quantize(x, codes, scales) -> None:
     """x f32 or bf16 [..., C]; codes uint8 [..., C/2] and scales uint8 [..., ceil(C/32)]: outputs."""
-    rows, cols = _mxfp4_rows(x, codes, scales)
-    _check("moe_mxfp4_quantize", lib().moe_mxfp4_quantize(_ptr(x), rows, cols, _act_dtype(x), _ptr(codes), _ptr(scales),
-                                                          _stream(x.device)))
+    rows, cols, px, pc, ps = _mxfp4_rows(x, codes, scales)
+    _check("moe_mxfp4_quantize", lib().moe_mxfp4_quantize(px, rows, cols, _act_dtype(x), pc, ps, _stream(x.device)))
 
 
 def moe_mxfp4_dequantize(codes, scales, x) -> None:
     """codes uint8 [..., C/2], scales uint8 [..., ceil(C/32)]; x f32 or bf16 [..., C]: output."""
-    rows, cols = _mxfp4_rows(x, codes, scales)
-    _check("moe_mxfp4_dequantize", lib().moe_mxfp4_dequantize(_ptr(codes), _ptr(scales), rows, cols, _act_dtype(x), _ptr(x),
-                                                              _stream(x.device)))
+    rows, cols, px, pc, ps = _mxfp4_rows(x, codes, scales)
+    _check("moe_mxfp4_dequantize", lib().moe_mxfp4_dequantize(pc, ps, rows, cols, _act_dtype(x), px, _stream(x.device)))
 
 
 def moe_mxfp4_pack(codes, scales) -> torch.Tensor:
@@ -426,36 +432,31 @@ def alloc_mxfp4_workspace(shape: MoeShape, device) -> torch.Tensor:
 _DTYPES = {MOE_F32: torch.float32, MOE_BF16: torch.bfloat16}
 
 
-def _mxfp4_call(shape: MoeShape, weights: Mxfp4Weights, x, y, topk_idx, topk_gate, workspace) -> None:
+def _mxfp4_call(shape: MoeShape, weights: Mxfp4Weights, x, y, topk_idx, topk_gate, workspace):
+    """Pointers of x, y, topk_idx, topk_gate and workspace, and the bytes of the last"""
     if (shape.n_experts, shape.d_model, shape.d_ff) != (weights.E, weights.d, weights.F):
         raise ValueError(f"shape of {shape.n_experts} experts {shape.d_model} / {shape.d_ff}, weights of "
                          f"{weights.E} experts {weights.d} / {weights.F}")
-    T, k, dtype = shape.n_tokens, shape.top_k, _DTYPES.get(shape.act_dtype)
-    _want("x", x, dtype, T, shape.d_model)
-    _want("y", y, dtype, T, shape.d_model)
-    if topk_idx is not None:
-        _want("topk_idx", topk_idx, torch.int32, T, k)
-    if topk_gate is not None:
-        _want("topk_gate", topk_gate, torch.float32, T, k)
-    _same_device(x, y, topk_idx, topk_gate, workspace, weights.tensors["gate"])
+    T, dtype, at = shape.n_tokens, _DTYPES.get(shape.act_dtype), x.get_device()
+    rows, picks = (T, shape.d_model), (T, shape.top_k)
+    if workspace is not None and workspace.get_device() != at or weights.tensors["gate"].get_device() != at:
+        raise ValueError("weights or workspace on another device than x")
+    return (_arg("x", x, dtype, rows, at), _arg("y", y, dtype, rows, at), _arg("topk_idx", topk_idx, torch.int32, picks, at),
+            _arg("topk_gate", topk_gate, torch.float32, picks, at), _ptr(workspace),
+            0 if workspace is None else workspace.numel() * workspace.element_size())
 
 
 def moe_mxfp4_experts(shape: MoeShape, weights: Mxfp4Weights, x, topk_idx, topk_gate, y, workspace) -> None:
     """The layer from the picks on: x [T,d], topk_idx int32 [T,k], topk_gate f32 [T,k]; y [T,d]: output."""
-    _mxfp4_call(shape, weights, x, y, topk_idx, topk_gate, workspace)
-    _check("moe_mxfp4_experts", lib().moe_mxfp4_experts(
-        C.byref(shape), C.byref(weights.struct), _ptr(x), _ptr(topk_idx), _ptr(topk_gate), _ptr(y), _ptr(workspace),
-        workspace.numel() * workspace.element_size(), _stream(x.device)))
+    px, py, pi, pg, pw, n = _mxfp4_call(shape, weights, x, y, topk_idx, topk_gate, workspace)
+    _check("moe_mxfp4_experts", lib().moe_mxfp4_experts(C.byref(shape), C.byref(weights.struct), px, pi, pg, py, pw, n,
+                                                        _stream(x.device)))
 
 
 def moe_mxfp4_forward(shape: MoeShape, config: RouteConfig, weights: Mxfp4Weights, x, y, topk_idx=None, topk_gate=None,
                       logits=None, workspace=None) -> None:
     """Router, picks and experts: x [T,d]; y [T,d], and topk_idx, topk_gate, logits f32 [T,E] or None: outputs."""
-    _mxfp4_call(shape, weights, x, y, topk_idx, topk_gate, workspace)
-    if logits is not None:
-        _want("logits", logits, torch.float32, shape.n_tokens, shape.n_experts)
-        _same_device(x, logits)
-    _check("moe_mxfp4_forward", lib().moe_mxfp4_forward(
-        C.byref(shape), C.byref(config), C.byref(weights.struct), _ptr(x), _ptr(y), _ptr(topk_idx), _ptr(topk_gate),
-        _ptr(logits), _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
-        _stream(x.device)))
+    px, py, pi, pg, pw, n = _mxfp4_call(shape, weights, x, y, topk_idx, topk_gate, workspace)
+    pl = _arg("logits", logits, torch.float32, (shape.n_tokens, shape.n_experts), x.get_device())
+    _check("moe_mxfp4_forward", lib().moe_mxfp4_forward(C.byref(shape), C.byref(config), C.byref(weights.struct), px, py, pi, pg, pl,
+                                                        pw, n, _stream(x.device)))

@@ -283,3 +283,17 @@ def test_more_groups_of_rows_than_a_grid_has_in_its_second_dimension():
     for part in (slice(0, 50), slice(T // 2, T // 2 + 50), slice(T - 50, T)):
         ref, tol = oo.experts(x[part].double().cpu().numpy(), exact, np.zeros((50, 1), np.int32), np.ones((50, 1)), False, 2.0 ** -8)
         assert (np.abs(y[part].double().cpu().numpy() - ref) <= tol).all()
+
+
+@pytest.mark.parametrize("rows,cols,dtype", [(70000, 960, "bf16"), (34000, 1000, "f32")])
+def test_quantize_large(rows, cols, dtype):
+    # above 128 MB, whole blocks and a short last one: the first and the last rows, and rows in between
+    x = (torch.randn(rows, cols, device=dev()) * torch.exp(torch.randn(rows, 1, device=dev()))).to(DTYPES[dtype])
+    codes, scales = _quantize(x)
+    for part in (slice(0, 40), slice(rows // 2, rows // 2 + 40), slice(rows - 40, rows)):
+        c, b = oo.quantize(x[part].double().cpu().numpy())
+        assert np.array_equal(codes[part].cpu().numpy(), oo.pack_nibbles(c))
+        assert np.array_equal(scales[part].cpu().numpy(), b)
+    y = torch.empty_like(x)
+    pkg.moe_mxfp4_dequantize(codes, scales, y)
+    assert ((y.float() - x.float()).abs() <= x.float().abs().amax(1, keepdim=True) * 0.25).all()  # (a step of the grid's upper end, or the cut at 6)
