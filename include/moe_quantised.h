@@ -27,7 +27,7 @@ extern "C" {
  * its group's rank.  Where fewer than k eligible experts are left, switched-off ones of the kept
  * groups follow, in ascending order, with gate 0.  Other non-finite logits: unspecified values,
  * picks inside [0, E).
- * Keys are compared as their exact values would be, up to 2^-48: near ties are decided in 64 bits.
+ * Near ties are decided by keys in 64 bits.
  */
 enum { MOE_SCORE_SOFTMAX = 0, MOE_SCORE_SIGMOID = 1 };
 
@@ -80,8 +80,8 @@ MOE_API int moe_route_scored_backward(const moe_route_config* config, int32_t n_
 /* x [rows, cols] (act_dtype) -> codes [rows, cols / 2], scales [rows, ceil(cols / 32)].  codes: 4-byte aligned. */
 MOE_API int moe_mxfp4_quantize(const void* x, int64_t rows, int32_t cols, int32_t act_dtype,
                                uint8_t* codes, uint8_t* scales, void* stream);
-/* The values that codes and scales stand for, in act_dtype (both hold them exactly, bf16 below 2^-126 and
- * fp32 there too).  A block of b = 255 gives NaN. */
+/* The values that codes and scales stand for, in act_dtype, exactly (subnormal ones too; above the type's range
+ * infinity).  A block of b = 255 gives NaN. */
 MOE_API int moe_mxfp4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows, int32_t cols,
                                  int32_t act_dtype, void* x, void* stream);
 
