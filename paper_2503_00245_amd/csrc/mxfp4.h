@@ -108,20 +108,14 @@ __device__ __forceinline__ void mx_store_hidden(const float (&f)[8], char* __res
     *reinterpret_cast<unsigned*>(codes + unit * kMxCodes + ((c & 1) * 2 + n) * 1024 + at * 16 + (lane >> 4) * 4) = mx_codes8(f, b);
     if (lane < 16) scales[unit * kMxScales + at * 4 + (c & 1) * 2 + n] = (char)b;
 }
-// The same of a product that is not quantised: eight neighbours of row 32 sb + 16 n + lane % 16 of [.., N]
-template <typename T>
+// The same of a product that is not quantised: eight neighbours of row 32 sb + 16 n + lane % 16 of fp32 [.., N].  (fp32 whatever the
+// activations' type: rounded to bf16 here, rows of experts that cancel would leave their roundings in the gated sum.)
 __device__ __forceinline__ void mx_store_rows(const float (&f)[8], char* __restrict__ out, int N, int sb, int n, int fb, int lane) {
     const int col = fb * 32 + (lane >> 4) * 8;
     if (col >= N) return;
-    T* y = reinterpret_cast<T*>(out) + ((size_t)sb * 32 + n * 16 + (lane & 15)) * N + col;
-    typedef typename Store<T>::vec_t vec_t;
-#pragma unroll
-    for (int h = 0; h < 8; h += Store<T>::VEC) {
-        vec_t o;
-#pragma unroll
-        for (int j = 0; j < Store<T>::VEC; ++j) o[j] = Store<T>::from_f32(f[h + j]);
-        *reinterpret_cast<vec_t*>(y + h) = o;
-    }
+    f32x4* const y = reinterpret_cast<f32x4*>(reinterpret_cast<float*>(out) + ((size_t)sb * 32 + n * 16 + (lane & 15)) * N + col);
+    y[0] = f32x4{f[0], f[1], f[2], f[3]};
+    y[1] = f32x4{f[4], f[5], f[6], f[7]};
 }
 
 // D (16 x 16, fp32) += A (16 x 128) B^T; SA, SB: which byte of the dwords sa, sb scales the lane's 32 codes
@@ -163,10 +157,10 @@ inline bool mx_few(const moe_shape& s) { return (long long)s.n_tokens * s.top_k 
 int launch_mx_few(const moe_shape& s, const moe_mxfp4_weights& w, const void* x, const int32_t* idx, const float* gate, void* y, const MxLayout& l, char* ws,
                   hipStream_t st);
 // Products of some rows an expert (mxfp4_stream.hip), the same arguments
-int launch_mx_stream(bool swiglu, int act_dtype, const void* w0, const void* w1, const char* a, char* out, const int32_t* starts, int P, int E,
+int launch_mx_stream(bool swiglu, const void* w0, const void* w1, const char* a, char* out, const int32_t* starts, int P, int E,
                      int all_blocks, int N, int K, hipStream_t st);
-// Products of many rows (mxfp4_gemm.hip): swiglu: hidden rows (w0 gate, w1 up), else rows of act_dtype (w0).  bs: rows of a tile, 256, 128 or 64
-int launch_mx_gemm(bool swiglu, int act_dtype, const void* w0, const void* w1, const char* a, char* out, const int32_t* starts, int P, int E,
+// Products of many rows (mxfp4_gemm.hip): swiglu: hidden rows (w0 gate, w1 up), else rows in fp32 (w0).  bs: rows of a tile, 256, 128 or 64
+int launch_mx_gemm(bool swiglu, const void* w0, const void* w1, const char* a, char* out, const int32_t* starts, int P, int E,
                    int all_blocks, int N, int K, int bs, hipStream_t st);
 int launch_router_logits(const moe_shape& s, const void* x, const float* rw, const float* rb, float* logits, hipStream_t st);
 int launch_route_scored(const moe_route_config& c, int T, int E, int k, const float* logits, const float* bias, int32_t* idx, float* gate,

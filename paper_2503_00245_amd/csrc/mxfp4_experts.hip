@@ -85,9 +85,11 @@ __global__ __launch_bounds__(kRowThreads) void mx_rows_kernel(const T* __restric
 }
 
 // ---- combine --------------------------------------------------------------------------------------------------------
-// y_t = sum_j g_tj (row of pair (t, j)) (+ x_t), in fp32 and ascending j; a lane takes one 16-byte piece of a row.
+// y_t = sum_j g_tj (row of pair (t, j)) (+ x_t), of rows in fp32, in fp32 and ascending j, rounded once; a lane takes one 16-byte piece
+// of a row of y.  (Rows in bf16 are half the bytes here and for the product that writes them: 16384 tokens of 2048 / 5632, us, down 204 and this 34 with
+// them, 236 and 54 now, a layer 7 % longer; 2048 tokens 130 and 136.)
 template <typename T>
-__global__ __launch_bounds__(kThreads) void mx_combine_kernel(const T* __restrict__ rows, const int32_t* __restrict__ slot, const float* __restrict__ gate,
+__global__ __launch_bounds__(kThreads) void mx_combine_kernel(const float* __restrict__ rows, const int32_t* __restrict__ slot, const float* __restrict__ gate,
                                                               const T* __restrict__ residual, T* __restrict__ y, int pieces, int k, long long all, int last_row) {
     typedef Store<T> S;
     for (long long i = blockIdx.x * (long long)kThreads + threadIdx.x; i < all; i += gridDim.x * (long long)kThreads) {
@@ -101,7 +103,7 @@ __global__ __launch_bounds__(kThreads) void mx_combine_kernel(const T* __restric
         for (int j0 = 0; j0 < k; j0 += 4) {
             int r[4];
             float w[4];
-            typename S::vec_t v[4];
+            f32x4 v[4][S::VEC / 4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 r[j] = slot[t * k + min(j0 + j, k - 1)];
@@ -110,13 +112,16 @@ __global__ __launch_bounds__(kThreads) void mx_combine_kernel(const T* __restric
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 r[j] = min(max(r[j], 0), last_row);  // (in range for picks of no expert as well)
-                if (j0 + j < k) v[j] = *reinterpret_cast<const typename S::vec_t*>(rows + r[j] * d + at);
+                if (j0 + j < k) {
+#pragma unroll
+                    for (int q = 0; q < S::VEC / 4; ++q) v[j][q] = *reinterpret_cast<const f32x4*>(rows + r[j] * d + at + 4 * q);
+                }
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 if (j0 + j >= k) break;
 #pragma unroll
-                for (int q = 0; q < S::VEC; ++q) f[q] = fmaf(w[j], S::get(v[j], q), f[q]);
+                for (int q = 0; q < S::VEC; ++q) f[q] = fmaf(w[j], v[j][q / 4][q % 4], f[q]);
             }
         }
         if (residual) {
@@ -153,7 +158,7 @@ MxLayout mx_layout(const moe_shape& s) {
     l.sort = take(P > kMxKeyPairs ? sizeof(int32_t) * 256 * s.n_experts : 0);  // (launch_permute: up to 256 counts an expert)
     l.xq = take((size_t)l.blocks * mx_units(s.d_model) * (kMxCodes + kMxScales));
     l.hq = take((size_t)l.blocks * mx_units(s.d_ff) * (kMxCodes + kMxScales));
-    l.y = take((size_t)l.blocks * 32 * s.d_model * elt_size(s.act_dtype));
+    l.y = take((size_t)l.blocks * 32 * s.d_model * sizeof(float));
     l.total = cur;
     return l;
 }
@@ -161,9 +166,9 @@ MxLayout mx_layout(const moe_shape& s) {
 // Rows of a tile of a product of P rows in E groups: 32 (mxfp4_stream.hip), 64, 128 or 256 (mxfp4_gemm.hip), whichever is the shortest by what
 // they measured, in us.  Tiles: rounds of 256 workgroups, a round so much a tile and so much a unit of K.  Streamed: so much of a CU for 32 rows of
 // weights by 32.  In no case less than the weights at 4.6 TB/s.  How unevenly the rows are spread the host does not know: half a tile more
-// an expert.  Whole layers, us, this choice / the best of eight pairs of choices: 2048 / 5632, 2 of 8 experts, 200 tokens 56.8 / 54.0, 400 63.8 / 63.8, 800
-// 75.5 / 75.5, 1200 94.1 / 89.6, 2048 132.2 / 132.2; 1024 / 2816, 256 tokens 24.2 / 23.9, 2048 55.2 / 55.2; 1440 / 3840, 777 tokens 51.9 / 51.9; 432 / 1152,
-// 300 tokens 15.9 / 15.9.
+// an expert.  Whole layers, us, weights cold, this choice / the best of the sixteen pairs of choices: 2048 / 5632, 2 of 8 experts, 64 tokens 46.0 / 41.9,
+// 200 tokens 52.9 / 52.5, 400 63.2 / 63.2, 800 76.7 / 73.1, 1200 95.7 / 95.7, 2048 136.3 / 135.9, 4096 225.3 / 223.7; 1024 / 2816, 256 tokens 24.5 / 24.2, 2048
+// 58.9 / 58.9, 4 of 16 experts, 24 tokens 27.1 / 27.0, 4 of 32 experts, 2048 tokens 111.9 / 104.7; 1440 / 3840, 777 tokens 53.0 / 52.9; 432 / 1152, 300 tokens 15.1 / 15.1.
 static int mx_tile_rows(bool swiglu, int P, int E, int N, int K) {
     const double rows = (double)P / E, units = mx_units(K), weights_mb = 0.53e-6 * N * (double)K * (swiglu ? 2 : 1) * std::min(P, E);
     auto groups = [&](int of) { return std::min((double)P, E * std::max(1.0, rows / of + 0.5)); };
@@ -201,8 +206,8 @@ static int experts(const moe_shape& s, const moe_mxfp4_weights& w, const T* x, c
                        starts, slot, ws + l.xq, ws + l.xq + (size_t)l.blocks * units * kMxCodes);
     auto product = [&](bool swiglu, const void* w0, const void* w1, char* a, char* out, int N, int K) {
         const int rows = mx_tile_rows(swiglu, P, E, N, K);
-        return rows <= 32 ? launch_mx_stream(swiglu, s.act_dtype, w0, w1, a, out, starts, P, E, l.blocks, N, K, st)
-                          : launch_mx_gemm(swiglu, s.act_dtype, w0, w1, a, out, starts, P, E, l.blocks, N, K, rows, st);
+        return rows <= 32 ? launch_mx_stream(swiglu, w0, w1, a, out, starts, P, E, l.blocks, N, K, st)
+                          : launch_mx_gemm(swiglu, w0, w1, a, out, starts, P, E, l.blocks, N, K, rows, st);
     };
     int rc = product(true, w.gate, w.up, ws + l.xq, ws + l.hq, F, d);
     if (rc == MOE_OK) rc = product(false, w.down, nullptr, ws + l.hq, ws + l.y, d, F);
@@ -210,7 +215,7 @@ static int experts(const moe_shape& s, const moe_mxfp4_weights& w, const T* x, c
     const int pieces = d / Store<T>::VEC;
     const long long all = (long long)s.n_tokens * pieces;
     hipLaunchKernelGGL(mx_combine_kernel<T>, dim3((unsigned)std::min<long long>((all + kThreads - 1) / kThreads, 1 << 20)), dim3(kThreads), 0, st,
-                       reinterpret_cast<const T*>(ws + l.y), slot, gate, (s.flags & MOE_FLAG_RESIDUAL) ? x : nullptr, y, pieces, s.top_k, all, l.blocks * 32 - 1);
+                       reinterpret_cast<const float*>(ws + l.y), slot, gate, (s.flags & MOE_FLAG_RESIDUAL) ? x : nullptr, y, pieces, s.top_k, all, l.blocks * 32 - 1);
     return launch_status();
 }
 

@@ -35,7 +35,7 @@ constexpr int kSplitSlots = 32;  // one workgroup per CU
 struct MxGemmArgs {
     const char *w0, *w1;  // packed weights (w1: up, with SWIGLU)
     const char* a;        // rows of activations in the layout of mxfp4.h: codes, then scales
-    char* out;            // SWIGLU: rows of the next product in that layout; else rows [.., N] of T
+    char* out;            // SWIGLU: rows of the next product in that layout; else rows [.., N] in fp32
     const int32_t* starts;  // [E + 1] first block of 32 rows of every expert
     int E, all_blocks, N, K;
 };
@@ -44,7 +44,7 @@ struct MxGemmArgs {
 constexpr int mx_stage(int blocks) { return (8 + blocks) * kMxCodes + (8 + (blocks + 3) / 4 * 4) * kMxScales; }
 
 // BS: rows of activations of a tile; NST: units in LDS
-template <int BS, int NST, bool SWIGLU, typename T>
+template <int BS, int NST, bool SWIGLU>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void mx_gemm_kernel(const MxGemmArgs g) {
     constexpr int WM = BS == 256 ? 2 : 4, WS = 8 / WM;  // waves along the weights, along the activations
     constexpr int WB = 8 / WM, SB = BS / 32 / WS;       // blocks of 32 rows of a wave
@@ -237,13 +237,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                     f[j] = SWIGLU ? (fb < fbs ? silu_f32(z) * acc[(b + WB / 2) % WB][i][j / 4][n][j % 4] : 0.f) : z;  // (beyond: the last block's again)
                 }
                 if constexpr (SWIGLU) mx_store_hidden(f, g.out, out_scales, out_units, sb, n, fb, lane);
-                else mx_store_rows<T>(f, g.out, g.N, sb, n, fb, lane);
+                else mx_store_rows(f, g.out, g.N, sb, n, fb, lane);
             }
         }
     }
 }
 
-template <int BS, int NST, bool SWIGLU, typename T>
+template <int BS, int NST, bool SWIGLU>
 int launch_tile(const MxGemmArgs& g, int P, hipStream_t st) {
     constexpr int SBLK = BS / 32;
     constexpr size_t lds = (size_t)NST * mx_stage(SBLK);
@@ -251,28 +251,26 @@ int launch_tile(const MxGemmArgs& g, int P, hipStream_t st) {
     constexpr int OUT_BLOCKS = SWIGLU ? 4 : 8;
     const int out_blocks = SWIGLU ? mx_units(g.N) * (kMxUnit / 32) : mx_blocks(g.N);
     const int tiles = m_tiles_bound(P, g.E, BS) * ((out_blocks + OUT_BLOCKS - 1) / OUT_BLOCKS);
-    auto kern = mx_gemm_kernel<BS, NST, SWIGLU, T>;
+    auto kern = mx_gemm_kernel<BS, NST, SWIGLU>;
     static std::atomic<uint64_t> allowed{0};
     if (allow_dynamic_lds(reinterpret_cast<const void*>(kern), lds, allowed) != MOE_OK) return MOE_ERR_LAUNCH;
     hipLaunchKernelGGL(kern, dim3(find_tile_grid(tiles, kSplitSlots)), dim3(kThreads), lds, st, g);
     return launch_status();
 }
 
-template <bool SWIGLU, typename T>
+template <bool SWIGLU>
 int launch_product(const MxGemmArgs& g, int P, int bs, hipStream_t st) {
-    if (bs == 256) return launch_tile<256, 2, SWIGLU, T>(g, P, st);
-    if (bs == 128) return launch_tile<128, 3, SWIGLU, T>(g, P, st);
-    return launch_tile<64, 3, SWIGLU, T>(g, P, st);
+    if (bs == 256) return launch_tile<256, 2, SWIGLU>(g, P, st);
+    if (bs == 128) return launch_tile<128, 3, SWIGLU>(g, P, st);
+    return launch_tile<64, 3, SWIGLU>(g, P, st);
 }
 
 }  // namespace
 
-int launch_mx_gemm(bool swiglu, int act_dtype, const void* w0, const void* w1, const char* a, char* out, const int32_t* starts, int P, int E,
+int launch_mx_gemm(bool swiglu, const void* w0, const void* w1, const char* a, char* out, const int32_t* starts, int P, int E,
                    int all_blocks, int N, int K, int bs, hipStream_t st) {
     const MxGemmArgs g{static_cast<const char*>(w0), static_cast<const char*>(w1), a, out, starts, E, all_blocks, N, K};
-    if (swiglu) return launch_product<true, bf16_t>(g, P, bs, st);  // (its output is codes, whatever the type)
-    if (act_dtype == MOE_F32) return launch_product<false, float>(g, P, bs, st);
-    return launch_product<false, bf16_t>(g, P, bs, st);
+    return swiglu ? launch_product<true>(g, P, bs, st) : launch_product<false>(g, P, bs, st);
 }
 
 }  // namespace moe

@@ -13,7 +13,7 @@ namespace {
 constexpr int kWaves = 4;
 
 // ONCE: most experts have one group of rows, and the weights need not stay in the caches (2048 / 5632, 32 tokens 46.1 -> 43.7 us a layer)
-template <bool SWIGLU, bool ONCE, typename T>
+template <bool SWIGLU, bool ONCE>
 __global__ __launch_bounds__(kWaves* kWave) void mx_stream_kernel(ptr_arg a_starts, ptr_arg a_w0, ptr_arg a_w1, ptr_arg a_rows, int E, int N, int K, int all_blocks,
                                                                   ptr_arg a_out) {
     constexpr int M = SWIGLU ? 2 : 1, NT = 2;  // matrices, tiles of 16 rows
@@ -77,25 +77,24 @@ __global__ __launch_bounds__(kWaves* kWave) void mx_stream_kernel(ptr_arg a_star
 #pragma unroll
         for (int j = 0; j < 8; ++j) f[j] = SWIGLU ? silu_f32(sum[0][j / 4][j % 4]) * sum[M - 1][j / 4][j % 4] : sum[0][j / 4][j % 4];
         if constexpr (SWIGLU) mx_store_hidden(f, out, out + (size_t)all_blocks * out_units * kMxCodes, out_units, sb, n, fb, lane);
-        else mx_store_rows<T>(f, out, N, sb, n, fb, lane);
+        else mx_store_rows(f, out, N, sb, n, fb, lane);
     }
 }
 
 }  // namespace
 
-int launch_mx_stream(bool swiglu, int act_dtype, const void* w0, const void* w1, const char* a, char* out, const int32_t* starts, int P, int E,
+int launch_mx_stream(bool swiglu, const void* w0, const void* w1, const char* a, char* out, const int32_t* starts, int P, int E,
                      int all_blocks, int N, int K, hipStream_t st) {
     const dim3 grid(swiglu ? mx_units(N) * (kMxUnit / 32) : mx_blocks(N), m_tiles_bound(P, E, 32));
     auto launch = [&](auto kern) {
         hipLaunchKernelGGL(kern, grid, dim3(kWaves * kWave), 0, st, as_arg(starts), as_arg(w0), as_arg(w1), as_arg(a), E, N, K, all_blocks, as_arg(out));
         return launch_status();
     };
-    auto launch_type = [&](auto once) {
+    auto launch_of = [&](auto once) {
         constexpr bool O = decltype(once)::value;
-        if (swiglu) return launch(mx_stream_kernel<true, O, bf16_t>);  // (its output is codes, whatever the type)
-        return act_dtype == MOE_F32 ? launch(mx_stream_kernel<false, O, float>) : launch(mx_stream_kernel<false, O, bf16_t>);
+        return swiglu ? launch(mx_stream_kernel<true, O>) : launch(mx_stream_kernel<false, O>);
     };
-    return P <= 32 * E ? launch_type(std::true_type{}) : launch_type(std::false_type{});
+    return P <= 32 * E ? launch_of(std::true_type{}) : launch_of(std::false_type{});
 }
 
 }  // namespace moe

@@ -1,0 +1,41 @@
+"""The products of experts in microscaled 4-bit floating point and the sum of their rows, on the GPU, against plain implementations in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2503_00245_amd as pkg
+from tests import operators_oracle as oo
+from tests.test_mxfp4_gpu import DTYPES, _layer, _run, dev
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("T", [1, 4, 5, 40, 300, 1500])
+def test_the_gated_sum_is_of_rows_that_are_not_rounded(T):
+    # Experts in pairs: the second one is the first with its down product's signs turned, but for one column in 64, so that a sum is an eighth to a
+    # quarter of its two addends: what rounding those to bf16 would leave (2^-9 of them each) is above the result's own rounding
+    # (2^-8 of an eighth).  The bound has no such rounding: sums in fp32 and steps of the hidden rows' 4 bits, then one rounding of y.
+    print("sum", T, flush=True)
+    E, d, F, k = 8, 128, 256, 2
+    rng = np.random.default_rng(T)
+    w, exact = _layer(rng, E, d, F)
+    for n in ("gate", "up"):
+        for part in ("_codes", "_scales"):
+            w[n + part][1::2] = w[n + part][0::2]
+    for m in (0, 1):
+        exact[m][1::2] = exact[m][0::2]
+    kept = np.arange(F) % 64 == 5
+    turn = torch.from_numpy(np.where(kept[0::2], 0, 0x08) | np.where(kept[1::2], 0, 0x80)).to(torch.uint8).to(dev())
+    w["down_codes"][1::2] = w["down_codes"][0::2] ^ turn
+    w["down_scales"][1::2] = w["down_scales"][0::2]
+    exact[2][1::2] = exact[2][0::2] * np.where(kept, 1.0, -1.0)
+    first = rng.integers(0, E // 2, (T, 1)) * 2
+    idx = np.concatenate([first, first + 1], 1).astype(np.int32)
+    gate = np.ones((T, k), np.float32)
+    x = torch.from_numpy(rng.standard_normal((T, d)).astype(np.float32)).bfloat16().to(dev())
+    y = _run(x, w, torch.from_numpy(idx).to(dev()), torch.from_numpy(gate).to(dev()), E, k, d, F, "bf16", False)
+    ref, tol = oo.experts(x.double().cpu().numpy(), exact, idx, gate.astype(np.float64), False, 2.0 ** -24)
+    tol = tol * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(ref)
+    err = np.abs(y.double().cpu().numpy() - ref)
+    assert np.isfinite(err).all()
+    assert (err <= tol).all(), (err / np.maximum(tol, 1e-300)).max()
