@@ -17,11 +17,10 @@
 // Measured and not adopted: tiles one after the other in a workgroup, the fills running on into the next (447 and 204, 477 with a wait behind the stores); fills by the
 // group that reads (486 and 237: they stand before the reads); four waves of 128 by 128 and 256 accumulators, two thirds of the fragment reads
 // but one wave to a SIMD (607 and 251); fills every second product, column tiles in blocks of one, two or eight: none.
-#include <algorithm>
-
 #include "gemm.h"
 #include "lds_fill.h"
 #include "mxfp4.h"
+#include "mxfp4_plan.h"
 
 namespace moe {
 
@@ -30,7 +29,6 @@ namespace {
 #define INLINE __attribute__((always_inline))
 
 constexpr int kThreads = 512;
-constexpr int kSplitSlots = 32;  // one workgroup per CU
 
 struct MxGemmArgs {
     const char *w0, *w1;  // packed weights (w1: up, with SWIGLU)
@@ -51,7 +49,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     constexpr int SBLK = BS / 32;
     constexpr int W_BYTES = 8 * kMxCodes, S_BYTES = SBLK * kMxCodes;
     constexpr int SC_AT = W_BYTES + S_BYTES, STAGE = mx_stage(SBLK);
-    constexpr int OUT_BLOCKS = SWIGLU ? 4 : 8;          // blocks of 32 output columns of a tile
+    constexpr int OUT_BLOCKS = mx_tile_blocks(SWIGLU);  // blocks of 32 output columns of a tile
     constexpr int NF = 8 + SBLK + 1;                    // fill instructions of a wave of group 1 a unit
     static_assert(WB >= 2 && SB >= 1, "a gate block and its up block are one wave's");
     extern __shared__ __align__(16) char smem[];
@@ -59,16 +57,15 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int units = mx_units(g.K), fbs = mx_blocks(g.N), out_units = mx_units(g.N);
-    // SWIGLU: whole units of output columns, so that what pads the next product's K is written too
     const int out_blocks = SWIGLU ? out_units * (kMxUnit / 32) : fbs;
     int lo = 0, hi = 0, e, row0, row_end, nt;
     if (lane < g.E) {
         lo = g.starts[lane] * 32;
         hi = g.starts[lane + 1] * 32;
     }
-    auto n_tiles_of = [&](int) INLINE { return (out_blocks + OUT_BLOCKS - 1) / OUT_BLOCKS; };
+    auto n_tiles_of = [&](int) INLINE { return mx_column_tiles(SWIGLU, g.N); };
     // (blocks of four column tiles, and the tiles of a last round that is half full at most in two: 16384 tokens of 2048 / 5632, down 209 -> 203 us)
-    if (!find_tile<4, kSplitSlots>(lo, hi, g.E, BS, n_tiles_of, e, row0, row_end, nt)) return;
+    if (!find_tile<4, kMxSplitSlots>(lo, hi, g.E, BS, n_tiles_of, e, row0, row_end, nt)) return;
     const int sb0 = row0 >> 5, live_blocks = min(SBLK, (row_end - row0) >> 5);
     const int fb0 = nt * OUT_BLOCKS;
     const int grp = wave >> 2, wm = (wave % (2 * WM)) % WM, ws = wave / WM;
@@ -248,13 +245,11 @@ int launch_tile(const MxGemmArgs& g, int P, hipStream_t st) {
     constexpr int SBLK = BS / 32;
     constexpr size_t lds = (size_t)NST * mx_stage(SBLK);
     static_assert(lds <= 160 * 1024, "of a CU");
-    constexpr int OUT_BLOCKS = SWIGLU ? 4 : 8;
-    const int out_blocks = SWIGLU ? mx_units(g.N) * (kMxUnit / 32) : mx_blocks(g.N);
-    const int tiles = m_tiles_bound(P, g.E, BS) * ((out_blocks + OUT_BLOCKS - 1) / OUT_BLOCKS);
+    const int tiles = m_tiles_bound(P, g.E, BS) * mx_column_tiles(SWIGLU, g.N);
     auto kern = mx_gemm_kernel<BS, NST, SWIGLU>;
     static std::atomic<uint64_t> allowed{0};
     if (allow_dynamic_lds(reinterpret_cast<const void*>(kern), lds, allowed) != MOE_OK) return MOE_ERR_LAUNCH;
-    hipLaunchKernelGGL(kern, dim3(find_tile_grid(tiles, kSplitSlots)), dim3(kThreads), lds, st, g);
+    hipLaunchKernelGGL(kern, dim3(find_tile_grid(tiles, kMxSplitSlots)), dim3(kThreads), lds, st, g);
     return launch_status();
 }
 

@@ -5,6 +5,7 @@ import torch
 
 import paper_2503_00245_amd as pkg
 from tests import operators_oracle as oo
+from tests.mxfp4_cases import PATTERNS, TILED, picks
 from tests.test_mxfp4_gpu import DTYPES, _layer, _run, dev
 
 pytestmark = pytest.mark.gpu
@@ -39,3 +40,26 @@ def test_the_gated_sum_is_of_rows_that_are_not_rounded(T):
     err = np.abs(y.double().cpu().numpy() - ref)
     assert np.isfinite(err).all()
     assert (err <= tol).all(), (err / np.maximum(tol, 1e-300)).max()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,d,F,E,k,skew,hidden,down", TILED)
+def test_tiled_products(T, d, F, E, k, skew, hidden, down, dtype):
+    # (tests/test_mxfp4_plan_cpu.py holds the cases to the tiles that they name)
+    print("tiled", T, d, F, E, k, skew, hidden, down, dtype, flush=True)
+    rng = np.random.default_rng(T + d * 3 + F)
+    w, exact = _layer(rng, E, d, F)
+    idx, gate = picks(E, k, skew)
+    x = torch.from_numpy(rng.standard_normal((PATTERNS, d)).astype(np.float32)).to(DTYPES[dtype]).to(dev())
+    pattern = torch.arange(T, device=dev()) % PATTERNS
+    residual = F % 3 == 0
+    y = _run(x[pattern], w, torch.from_numpy(idx).to(dev())[pattern], torch.from_numpy(gate).to(dev())[pattern], E, k, d, F, dtype, residual)
+    half_step = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+    ref, tol = oo.experts(x.double().cpu().numpy(), exact, idx, gate.astype(np.float64), residual, 2.0 ** -24)
+    tol = tol * (1 + half_step) + half_step * np.abs(ref)
+    err = np.abs(y[:PATTERNS].double().cpu().numpy() - ref)
+    assert np.isfinite(err).all()
+    assert (err <= tol).all(), (err / np.maximum(tol, 1e-300)).max()
+    # a row's sums are formed in the same order wherever it lies in a tile: copies of a token have its bits
+    same = (y == y[:PATTERNS][pattern]).all(1)
+    assert same.all(), same.logical_not().nonzero()[:8].flatten().tolist()
