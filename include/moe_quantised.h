@@ -46,7 +46,7 @@ typedef struct moe_route_config {
  *   logits      [T, E] fp32 in
  *   select_bias [E]    fp32 or NULL (finite)
  *   topk_idx [T, k] int32, topk_gate [T, k] fp32 out; scores [T, E] fp32 out or NULL
- * 1 <= k <= groups_kept * E / n_groups, k <= 64, E <= MOE_ROUTE_MAX_EXPERTS, T E < 2^40.
+ * 1 <= k <= groups_kept * E / n_groups, k <= 64, E <= MOE_ROUTE_MAX_EXPERTS; any number of tokens.
  * Pointers of 4-byte elements need 4-byte alignment only.
  */
 MOE_API int moe_route_scored(const moe_route_config* config, int32_t n_tokens, int32_t n_experts, int32_t top_k,
@@ -77,7 +77,8 @@ MOE_API int moe_route_scored_backward(const moe_route_config* config, int32_t n_
  * and all of its values read back as NaN.
  */
 
-/* x [rows, cols] (act_dtype) -> codes [rows, cols / 2], scales [rows, ceil(cols / 32)].  codes: 4-byte aligned. */
+/* x [rows, cols] (act_dtype, 16-byte aligned) -> codes [rows, cols / 2], scales [rows, ceil(cols / 32)].  codes: 4-byte aligned; cols <= 2^24,
+ * rows cols <= 2^40. */
 MOE_API int moe_mxfp4_quantize(const void* x, int64_t rows, int32_t cols, int32_t act_dtype,
                                uint8_t* codes, uint8_t* scales, void* stream);
 /* The values that codes and scales stand for, in act_dtype, exactly (subnormal ones too; above the type's range
@@ -86,7 +87,8 @@ MOE_API int moe_mxfp4_dequantize(const uint8_t* codes, const uint8_t* scales, in
                                  int32_t act_dtype, void* x, void* stream);
 
 /* Layout of weights for moe_mxfp4_experts, made once: n_matrices row-major matrices [rows, cols] of codes and
- * scales as above, in the order in which the matrix units read them.  cols and rows: multiples of 8. */
+ * scales as above, in the order in which the matrix units read them.  cols and rows: multiples of 8, at most 2^24; the
+ * result (16-byte aligned) under 2^46 bytes. */
 MOE_API size_t moe_mxfp4_packed_bytes(int32_t n_matrices, int32_t rows, int32_t cols); /* 0 if invalid */
 MOE_API int moe_mxfp4_pack(const uint8_t* codes, const uint8_t* scales, int32_t n_matrices, int32_t rows,
                            int32_t cols, void* packed, void* stream);

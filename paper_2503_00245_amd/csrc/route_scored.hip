@@ -1,5 +1,6 @@
 // Routing from logits: scores by softmax or sigmoid, picks by score and bias inside the best groups, gates; and
 // the gradient of gates and scores with regard to the logits.  moe_quantised.h states the definition.
+#include <algorithm>
 #include <cmath>
 
 #include "mxfp4.h"
@@ -636,6 +637,18 @@ __global__ __launch_bounds__(kRouteWaves* kWave) void router_logits_kernel(const
     }
 }
 
+// launch(t0, n) for runs of up to kTokenRun tokens, one after the other: the 2^32 work items that a dimension of a grid may not reach are 2^26 tokens of
+// the gradient, 2^24 of the router's logits and 2^28 of the picks
+constexpr int kTokenRun = 1 << 23;
+template <typename L>
+int in_runs(int T, L launch) {
+    for (long long t0 = 0; t0 < T; t0 += kTokenRun) {
+        const int rc = launch((size_t)t0, (int)std::min<long long>(kTokenRun, T - t0));
+        if (rc != MOE_OK) return rc;
+    }
+    return MOE_OK;
+}
+
 // values a lane: a power of two
 template <typename L>
 int with_values(int E, L launch) {
@@ -670,29 +683,34 @@ int validate_route(const moe_route_config* c, int T, int E, int k) {
 
 int launch_route_scored(const moe_route_config& c, int T, int E, int k, const float* logits, const float* bias, int32_t* idx, float* gate,
                         float* scores, hipStream_t st) {
-    if (T == 0) return MOE_OK;
     // the order of keys is that of the logits, which fp32 holds exactly, unless there is a bias or a group's rank is a sum
     const bool by_logit = !bias && (c.n_groups == 1 || c.group_top == 1);
-    const RouteArgs g{logits, bias, idx, gate, scores, T, E, k, c.score, c.n_groups, c.groups_kept, c.group_top, c.renormalize, c.scale};
     constexpr int kTokens = kWaves * kWave / kTeam;
-    return with_team_values(E, [&](auto V) {
-        auto launch = [&](auto kern) {
-            hipLaunchKernelGGL(kern, dim3((T + kTokens - 1) / kTokens), dim3(kWaves * kWave), 0, st, g);
-            return launch_status();
-        };
-        constexpr int v = decltype(V)::value;
-        if (by_logit) return k <= kTeam ? launch(route_scored_kernel<v, 1, false>) : launch(route_scored_kernel<v, 4, false>);
-        return k <= kTeam ? launch(route_scored_kernel<v, 1, true>) : launch(route_scored_kernel<v, 4, true>);
+    return in_runs(T, [&](size_t t0, int n) {
+        const RouteArgs g{logits + t0 * E, bias, idx + t0 * k, gate + t0 * k, scores ? scores + t0 * E : nullptr, n, E, k, c.score, c.n_groups, c.groups_kept,
+                          c.group_top, c.renormalize, c.scale};
+        return with_team_values(E, [&](auto V) {
+            auto launch = [&](auto kern) {
+                hipLaunchKernelGGL(kern, dim3((n + kTokens - 1) / kTokens), dim3(kWaves * kWave), 0, st, g);
+                return launch_status();
+            };
+            constexpr int v = decltype(V)::value;
+            if (by_logit) return k <= kTeam ? launch(route_scored_kernel<v, 1, false>) : launch(route_scored_kernel<v, 4, false>);
+            return k <= kTeam ? launch(route_scored_kernel<v, 1, true>) : launch(route_scored_kernel<v, 4, true>);
+        });
     });
 }
 
 int launch_router_logits(const moe_shape& s, const void* x, const float* rw, const float* rb, float* logits, hipStream_t st) {
-    const dim3 grid((s.n_tokens + kRouteTok - 1) / kRouteTok), block(kRouteWaves * kWave);
-    if (s.act_dtype == MOE_F32)
-        hipLaunchKernelGGL(router_logits_kernel<float>, grid, block, 0, st, (const float*)x, rw, rb, s.d_model, s.n_experts, s.n_tokens, logits);
-    else
-        hipLaunchKernelGGL(router_logits_kernel<bf16_t>, grid, block, 0, st, (const bf16_t*)x, rw, rb, s.d_model, s.n_experts, s.n_tokens, logits);
-    return launch_status();
+    return in_runs(s.n_tokens, [&](size_t t0, int n) {
+        const dim3 grid((n + kRouteTok - 1) / kRouteTok), block(kRouteWaves * kWave);
+        auto launch = [&](auto kern, auto* rows) {
+            hipLaunchKernelGGL(kern, grid, block, 0, st, rows + t0 * s.d_model, rw, rb, s.d_model, s.n_experts, n, logits + t0 * s.n_experts);
+            return launch_status();
+        };
+        if (s.act_dtype == MOE_F32) return launch(router_logits_kernel<float>, static_cast<const float*>(x));
+        return launch(router_logits_kernel<bf16_t>, static_cast<const bf16_t*>(x));
+    });
 }
 
 }  // namespace moe
@@ -721,15 +739,19 @@ extern "C" int moe_route_scored_backward(const moe_route_config* config, int32_t
     const moe_route_config& c = *config;
     // four experts to a lane: rows of whole 16-byte pieces
     const bool four = n_experts >= 256 && n_experts % 4 == 0 && aligned16(logits) && aligned16(grad_scores) && aligned16(grad_logits);
-    return with_values(n_experts, [&](auto V) {
-        constexpr int v = decltype(V)::value;
-        auto launch = [&](auto kern) {
-            hipLaunchKernelGGL(kern, dim3((n_tokens + kWaves - 1) / kWaves), dim3(kWaves * kWave), 0, as_stream(stream), logits, topk_idx, grad_gate,
-                               grad_scores, grad_logits, n_tokens, n_experts, top_k, c.score, c.renormalize, c.scale);
-            return launch_status();
-        };
-        if constexpr (v >= 4)
-            if (four) return launch(route_scored_backward_kernel<v, true>);
-        return launch(route_scored_backward_kernel<v, false>);
+    const size_t E = n_experts, k = top_k;
+    return in_runs(n_tokens, [&](size_t t0, int n) {
+        return with_values(n_experts, [&](auto V) {
+            constexpr int v = decltype(V)::value;
+            auto launch = [&](auto kern) {
+                hipLaunchKernelGGL(kern, dim3((n + kWaves - 1) / kWaves), dim3(kWaves * kWave), 0, as_stream(stream), logits + t0 * E, topk_idx + t0 * k,
+                                   grad_gate + t0 * k, grad_scores ? grad_scores + t0 * E : nullptr, grad_logits + t0 * E, n, n_experts, top_k, c.score,
+                                   c.renormalize, c.scale);
+                return launch_status();
+            };
+            if constexpr (v >= 4)
+                if (four) return launch(route_scored_backward_kernel<v, true>);
+            return launch(route_scored_backward_kernel<v, false>);
+        });
     });
 }

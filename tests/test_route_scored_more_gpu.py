@@ -1,0 +1,51 @@
+"""Routing from logits and its gradient, on the GPU: numbers of tokens beyond a launch, near ties in single places, logits and gradients at the
+ends of their range."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2503_00245_amd as pkg
+from tests import operators_oracle as oo
+
+pytestmark = pytest.mark.gpu
+
+
+def dev():
+    return torch.device("cuda:0")
+
+
+# A dimension of a grid has less than 2^32 work items: 2^28 tokens of the picks' launch, 2^26 of the gradient's.
+def test_more_tokens_than_a_launch_has_picks_for():
+    T = (1 << 28) + 37
+    l = torch.randn(T, 2, device=dev())
+    idx, gate = torch.full((T, 1), -7, dtype=torch.int32, device=dev()), torch.full((T, 1), 7.0, device=dev())
+    pkg.moe_route_scored(pkg.make_route_config(renormalize=False), l, None, idx, gate)
+    right = bool((idx[:, 0] == (l[:, 1] > l[:, 0]).int()).all())  # (plain truth values: of tensors as long as these an assertion would make a text)
+    assert right
+    # the larger of two shares: 1 / (1 + e^-|l0 - l1|), from a difference rounded once
+    right = bool(((gate[:, 0] - torch.sigmoid((l[:, 0] - l[:, 1]).abs())).abs() <= 2.0 ** -20).all())
+    assert right
+
+
+def test_more_tokens_than_32_bits_round_up():
+    T = (1 << 31) - 1
+    l = torch.zeros(T, 1, device=dev())
+    idx, gate = torch.full((T, 1), -7, dtype=torch.int32, device=dev()), torch.full((T, 1), 7.0, device=dev())
+    pkg.moe_route_scored(pkg.make_route_config(scale=2.5), l, None, idx, gate)
+    ends = int(idx.min()), int(idx.max()), float(gate.min()), float(gate.max())
+    assert ends == (0, 0, 2.5, 2.5)
+
+
+def test_more_tokens_than_a_launch_has_gradients_for():
+    T = (1 << 26) + 37
+    l, dg = torch.randn(T, 2, device=dev()), torch.randn(T, 1, device=dev())
+    idx = (torch.rand(T, 1, device=dev()) < 0.5).int()
+    out = torch.full((T + 1, 2), 7.0, device=dev())
+    pkg.moe_route_scored_backward(pkg.make_route_config(pkg.SCORE_SIGMOID, renormalize=False, scale=2.0), l, idx, dg, None, out[:T])
+    right = bool((out[T] == 7).all())
+    assert right
+    s = torch.sigmoid(l.gather(1, idx.long()))
+    right = bool(((out[:T].gather(1, idx.long()) - 2 * dg * s * (1 - s)).abs() <= 2.0 ** -18 * dg.abs()).all())
+    assert right
+    right = not bool(out[:T].gather(1, 1 - idx.long()).any())
+    assert right
