@@ -109,7 +109,9 @@ typedef struct moe_mxfp4_weights {
  * The expert layer on such weights, from the picks on: with Q the rounding of a row to MXFP4 and back,
  *   h_tj = silu(W_gate,e Q(x_t)) * (W_up,e Q(x_t)),  e = topk_idx[t,j],
  *   y_t  = sum_j topk_gate[t,j] W_down,e Q(h_tj)   (+ x_t with MOE_FLAG_RESIDUAL).
- * Products and the gated sum are formed in fp32, from a token's rows as they are summed, and y is rounded once.  shape.rank must be 0, d_model and d_ff at most 2^18; the other limits are the layer's (E <= 64).
+ * Products and the gated sum are formed in fp32, from rows as they were summed, and y is rounded once.  shape.rank must be 0, d_model and
+ * d_ff at most 2^18, and tiles of 256 pairs by 128 hidden, or 256 output, columns fewer than 2^23 - 256 (T k F < 2^38 and T k d < 2^39, nearly: a
+ * workspace of 137 GB); the other limits are the layer's (E <= 64, T k < 2^24).
  *   x, y [T, d] act_dtype, y not aliasing x; topk_idx [T, k] int32 (pairs outside [0, E) leave their token's row unspecified),
  *   topk_gate [T, k] fp32; workspace: moe_mxfp4_workspace_bytes(shape), 16-byte aligned.
  */

@@ -209,6 +209,8 @@ static int validate_mx(const moe_shape* s) {
     if (s->flags & MOE_FLAG_SHARED_BASE) return MOE_ERR_INVALID;
     // (tiles are counted, and scales of a matrix found, in 32 bits)
     if (s->d_model > kMxMaxWidth || s->d_ff > kMxMaxWidth) return MOE_ERR_UNSUPPORTED;
+    const int P = s->n_tokens * s->top_k;
+    if (!mx_tiles_fit(true, P, s->n_experts, s->d_ff, 256) || !mx_tiles_fit(false, P, s->n_experts, s->d_model, 256)) return MOE_ERR_UNSUPPORTED;
     return s->rank ? MOE_ERR_UNSUPPORTED : MOE_OK;
 }
 static int validate_call(const moe_shape* s, const moe_mxfp4_weights* w, const void* x, const void* y) {

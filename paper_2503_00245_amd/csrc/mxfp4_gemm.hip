@@ -245,7 +245,7 @@ int launch_tile(const MxGemmArgs& g, int P, hipStream_t st) {
     constexpr int SBLK = BS / 32;
     constexpr size_t lds = (size_t)NST * mx_stage(SBLK);
     static_assert(lds <= 160 * 1024, "of a CU");
-    const int tiles = m_tiles_bound(P, g.E, BS) * mx_column_tiles(SWIGLU, g.N);
+    const int tiles = (int)mx_tiles(SWIGLU, P, g.E, g.N, BS);
     auto kern = mx_gemm_kernel<BS, NST, SWIGLU>;
     static std::atomic<uint64_t> allowed{0};
     if (allow_dynamic_lds(reinterpret_cast<const void*>(kern), lds, allowed) != MOE_OK) return MOE_ERR_LAUNCH;

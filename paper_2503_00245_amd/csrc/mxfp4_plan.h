@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <cmath>
 
+#include "gemm.h"
 #include "mxfp4.h"
 
 namespace moe {
@@ -15,6 +16,9 @@ __host__ __device__ constexpr int mx_column_tiles(bool swiglu, int N) {
     // (SWIGLU: whole units of output columns, so that what pads the next product's K is written too)
     return ((swiglu ? mx_units(N) * (kMxUnit / 32) : mx_blocks(N)) + mx_tile_blocks(swiglu) - 1) / mx_tile_blocks(swiglu);
 }
+// Tiles of so many rows that such a product can need, and whether that many workgroups of 512 threads are a launch: fewer than 2^32 work items
+inline long long mx_tiles(bool swiglu, int P, int E, int N, int rows) { return (long long)m_tiles_bound(P, E, rows) * mx_column_tiles(swiglu, N); }
+inline bool mx_tiles_fit(bool swiglu, int P, int E, int N, int rows) { return mx_tiles(swiglu, P, E, N, rows) + 8 * kMxSplitSlots < 1 << 23; }
 
 // Rows of a tile of a product of P rows in E groups: 32 (mxfp4_stream.hip), 64, 128 or 256 (mxfp4_gemm.hip), whichever is the shortest by what
 // they measured, in us.  Tiles: rounds of 256 workgroups, a round so much a tile and so much a unit of K.  Streamed: so much of a CU for 32 rows of
@@ -33,6 +37,7 @@ inline int mx_tile_rows(bool swiglu, int P, int E, int N, int K) {
         double tile, unit;
     } const tiles[] = {{64, swiglu ? 3.8 : 4.9, 0.55}, {128, 4.8, 0.85}, {256, swiglu ? 6.0 : 5.0, 1.52}};
     for (const auto& t : tiles) {
+        if (!mx_tiles_fit(swiglu, P, E, N, t.rows)) continue;  // (those of 256 rows do: validate_mx)
         const double rounds = std::ceil(groups(t.rows) * ((N + (swiglu ? 127 : 255)) / (swiglu ? 128 : 256)) / 256);
         const double us = std::max(rounds * (t.tile + units * t.unit), weights_mb / 4.6) + 2.5;
         if (us < best) best = us, choice = t.rows;

@@ -198,3 +198,16 @@ def test_plain_gradient_is_the_derivative():
                 p[0, e] += h
                 m[0, e] -= h
                 assert abs((f(p) - f(m)) / (2 * h) - got[0, e]) < 1e-8
+
+
+def test_experts_refuse_more_tiles_than_a_launch_has():
+    # 65536 groups of 256 rows by 128 tiles of 128 hidden, or of 256 output, columns: 2^23 workgroups of 512 threads
+    T, L = (1 << 24) - 1, pkg.lib()
+    for wide, d, F in ((True, 8, 1 << 14), (False, 8, (1 << 14) - 1024), (True, 1 << 15, 8), (False, (1 << 15) - 2048, 8)):
+        shape = pkg.make_shape(T, d, F, 1, 1)
+        n = pkg.moe_mxfp4_workspace_bytes(shape)
+        assert (n == 0) == wide
+        status = UNSUPPORTED if wide else WORKSPACE
+        assert L.moe_mxfp4_experts(C.byref(shape), C.byref(_weights()), OK, OK2, OK2, OK3, OK, 1, None) == status
+        cfg = pkg.make_route_config()
+        assert L.moe_mxfp4_forward(C.byref(shape), C.byref(cfg), C.byref(_weights()), OK, OK3, OK2, OK2, None, OK, 1, None) == status
