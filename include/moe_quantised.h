@@ -95,7 +95,7 @@ MOE_API int moe_mxfp4_pack(const uint8_t* codes, const uint8_t* scales, int32_t 
 
 /* Packed weights of one layer: gate, up from [E, F, d], down from [E, d, F].  The router's fields are
  * read by moe_mxfp4_forward alone: router_w [E, d] fp32, router_b [E] (of the logits) and select_bias [E]
- * fp32 or NULL. */
+ * fp32 or NULL.  All but the last two, which need 4-byte alignment only, are 16-byte aligned. */
 typedef struct moe_mxfp4_weights {
     const float* router_w;
     const float* router_b;

@@ -251,6 +251,8 @@ extern "C" int moe_mxfp4_forward(const moe_shape* shape, const moe_route_config*
     if (!weights->router_w || !aligned16(weights->router_w) || !workspace || !aligned16(workspace)) return MOE_ERR_INVALID;
     for (const void* p : {(const void*)topk_idx, (const void*)topk_gate, (const void*)logits})
         if (!aligned16(p)) return MOE_ERR_INVALID;
+    for (const float* p : {weights->router_b, weights->select_bias})  // (read value by value)
+        if (reinterpret_cast<uintptr_t>(p) & 3) return MOE_ERR_INVALID;
     const MxLayout l = mx_layout(*shape);
     if (workspace_bytes < l.total) return MOE_ERR_WORKSPACE;
     char* ws = static_cast<char*>(workspace);

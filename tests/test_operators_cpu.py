@@ -211,3 +211,11 @@ def test_experts_refuse_more_tiles_than_a_launch_has():
         assert L.moe_mxfp4_experts(C.byref(shape), C.byref(_weights()), OK, OK2, OK2, OK3, OK, 1, None) == status
         cfg = pkg.make_route_config()
         assert L.moe_mxfp4_forward(C.byref(shape), C.byref(cfg), C.byref(_weights()), OK, OK3, OK2, OK2, None, OK, 1, None) == status
+
+
+@pytest.mark.parametrize("name", ["router_b", "select_bias"])
+def test_the_whole_layer_refuses_biases_between_values(name):
+    sh, cfg, w = pkg.make_shape(8, 256, 512, 4, 2), pkg.make_route_config(), _weights()
+    for at, status in ((4098, INVALID), (4100, WORKSPACE)):  # (4-byte alignment is enough: the workspace is what is wrong then)
+        setattr(w, name, at)
+        assert pkg.lib().moe_mxfp4_forward(C.byref(sh), C.byref(cfg), C.byref(w), OK, OK3, OK2, OK2, None, OK, 1, None) == status
