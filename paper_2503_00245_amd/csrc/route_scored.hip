@@ -363,7 +363,7 @@ __global__ __launch_bounds__(kWaves* kWave) void route_scored_kernel(const Route
 #pragma unroll
                 for (int v = 0; v < V; ++v) key[v] = -INFINITY;
             }
-            unsure = team_min(e0 < E && !in && !out ? 0 : 1) == 0;
+            unsure = team_min(e0 < E && !in && !out ? 0 : 1) == 0 || (KEYS && !(gap < INFINITY));  // (sums beyond fp32 compare as equal)
         } else {
             // other groups: the keys of one token at a time through LDS, a group a lane
             float* s_key = s_logit[wave];
@@ -393,7 +393,7 @@ __global__ __launch_bounds__(kWaves* kWave) void route_scored_kernel(const Route
                 }
                 const unsigned long long open = __ballot(lane < g.G && from < g.kept), maybe = __ballot(lane < g.G && from >= g.kept && above < g.kept);
                 if (lane / kTeam == q) {
-                    unsure = maybe != 0;
+                    unsure = maybe != 0 || !(gap < INFINITY);
 #pragma unroll
                     for (int v = 0; v < V; ++v)
                         if (!(open >> min((e0 + v) / per, 63) & 1)) key[v] = -INFINITY;

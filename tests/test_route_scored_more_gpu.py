@@ -49,3 +49,21 @@ def test_more_tokens_than_a_launch_has_gradients_for():
     assert right
     right = not bool(out[:T].gather(1, 1 - idx.long()).any())
     assert right
+
+
+@pytest.mark.parametrize("E,groups", [(16, 4), (256, 8), (48, 4), (20, 4)])  # groups of whole lanes, and others
+@pytest.mark.parametrize("sigmoid", [False, True])
+def test_ranks_of_groups_beyond_the_range_of_fp32(E, groups, sigmoid):
+    # finite biases whose sums of two are not: keys far apart, every group's rank above the largest fp32 number
+    print("ranks", E, groups, sigmoid, flush=True)
+    T, k = 37, 4
+    rng = np.random.default_rng(E)
+    l = rng.standard_normal((T, E)).astype(np.float32)
+    for low, high in ((1.8e38, 3.3e38), (-3.3e38, -1.8e38)):
+        bias = rng.permutation(np.linspace(low, high, E)).astype(np.float32)
+        cfg = pkg.make_route_config(int(sigmoid), groups, 2, 2)
+        idx, gate = torch.empty(T, k, dtype=torch.int32, device=dev()), torch.empty(T, k, device=dev())
+        pkg.moe_route_scored(cfg, torch.from_numpy(l).to(dev()), torch.from_numpy(bias).to(dev()), idx, gate)
+        ref, ref_gate, _ = oo.route(l, bias, k, sigmoid, groups, 2, 2, True, 1.0)
+        assert np.array_equal(idx.cpu().numpy(), ref)
+        assert (np.abs(gate.double().cpu().numpy() - ref_gate) <= 2.0 ** -18).all()
