@@ -57,7 +57,8 @@ MOE_API int moe_route_scored(const moe_route_config* config, int32_t n_tokens, i
  * Gradient of moe_route_scored's gates and scores with regard to the logits, for the picks it made (the
  * picks themselves, and through them the bias and the groups, have none).  grad_gate [T, k] fp32;
  * grad_scores [T, E] fp32 or NULL; grad_logits [T, E] fp32 out, every element written.  Of a row whose
- * picked scores are all 0 the gates have no gradient.  Entries of topk_idx outside [0, E) are ignored; an
+ * picked scores are all 0 the gates have no gradient.  What the two hold for an expert that is switched
+ * off (an infinity or a NaN, say) plays no part.  Entries of topk_idx outside [0, E) are ignored; an
  * expert that is named twice counts twice.
  */
 MOE_API int moe_route_scored_backward(const moe_route_config* config, int32_t n_tokens, int32_t n_experts,

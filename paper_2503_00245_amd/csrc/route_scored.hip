@@ -528,9 +528,9 @@ __global__ __launch_bounds__(kWaves* kWave) void route_scored_backward_kernel(co
     };
     const int e_of = lane < k ? topk_idx[(size_t)t * k + lane] : -1;
     const bool named = (unsigned)e_of < (unsigned)E;
-    const float dg = named ? grad_gate[(size_t)t * k + lane] : 0.f;
+    float dg = named ? grad_gate[(size_t)t * k + lane] : 0.f;
     float pl = named ? row[e_of] : -INFINITY;
-    if (!(pl == pl)) pl = -INFINITY;
+    if (!(pl > -INFINITY)) pl = -INFINITY, dg = 0.f;  // (of a constant, whatever the gradient: 0 times an infinity would be a NaN of the row)
     // Without a gradient of the scores the logits that were not picked have none, and are not read, unless a softmax's sum couples them
     const bool all = grad_scores || !(renormalize || sigmoid);
     float l[V], ds[V], s[V], base = 0.f, den = 1.f;
@@ -542,7 +542,7 @@ __global__ __launch_bounds__(kWaves* kWave) void route_scored_backward_kernel(co
         float top = -INFINITY;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            if (!(l[v] == l[v])) l[v] = -INFINITY;
+            if (!(l[v] > -INFINITY)) l[v] = -INFINITY, ds[v] = 0.f;
             top = fmaxf(top, l[v]);
         }
         if (sigmoid) {

@@ -67,3 +67,34 @@ def test_ranks_of_groups_beyond_the_range_of_fp32(E, groups, sigmoid):
         ref, ref_gate, _ = oo.route(l, bias, k, sigmoid, groups, 2, 2, True, 1.0)
         assert np.array_equal(idx.cpu().numpy(), ref)
         assert (np.abs(gate.double().cpu().numpy() - ref_gate) <= 2.0 ** -18).all()
+
+
+@pytest.mark.parametrize("renorm", [False, True])
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("E,k", [(8, 3), (60, 6), (256, 8), (512, 64)])
+def test_gradients_of_experts_that_are_switched_off_play_no_part(E, k, sigmoid, renorm):
+    # the gradient of s log s at s = 0 is minus infinity: at an expert whose score is a constant it is of nothing
+    print("off", E, k, sigmoid, renorm, flush=True)
+    T = 41
+    rng = np.random.default_rng(E + k)
+    l = rng.standard_normal((T, E)).astype(np.float32)
+    dead = rng.random((T, E)) < 0.3
+    dead[::7] = True          # rows of nothing else
+    dead[1::7, : E - k + 1] = True  # ... and of fewer than k
+    l[dead] = np.where(rng.random((T, E)) < 0.5, -np.inf, np.nan)[dead].astype(np.float32)
+    idx, _, _ = oo.route(l, None, k, sigmoid, 1, 1, 1, renorm, 1.0)
+    dg, ds = rng.standard_normal((T, k)).astype(np.float32), rng.standard_normal((T, E)).astype(np.float32)
+    off_pick = np.take_along_axis(dead, idx.astype(np.int64), 1)
+    assert off_pick.any() and not off_pick.all()
+    out = []
+    for fill in (0.0, -np.inf, np.nan):
+        dg[off_pick], ds[dead] = fill, fill
+        for aux in (True, False):
+            g = torch.full((T, E), 7.0, device=dev())
+            pkg.moe_route_scored_backward(pkg.make_route_config(int(sigmoid), renormalize=renorm), torch.from_numpy(l).to(dev()), torch.from_numpy(idx).to(dev()),
+                                          torch.from_numpy(dg).to(dev()), torch.from_numpy(ds).to(dev()) if aux else None, g)
+            out.append(g)
+    for aux in (0, 1):
+        assert torch.isfinite(out[aux]).all()
+        assert not out[aux][torch.from_numpy(dead).to(dev())].any()
+        assert torch.equal(out[aux], out[2 + aux]) and torch.equal(out[aux], out[4 + aux])
