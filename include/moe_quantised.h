@@ -27,7 +27,10 @@ extern "C" {
  * its group's rank.  Where fewer than k eligible experts are left, switched-off ones of the kept
  * groups follow, in ascending order, with gate 0.  Other non-finite logits: unspecified values,
  * picks inside [0, E).
- * Near ties are decided by keys in 64 bits.
+ * Without a bias, and unless groups are ranked by two keys, keys are compared through their logits, exactly.
+ * Else near ties are decided by keys in 64 bits (in which sigmoid scores of logits above 37 are all 1, and tie).
+ * Keys in 32 bits decide what they can; a token of nearer ones (2^-18 of 1 + |c| for a softmax, 2^-21 for a
+ * sigmoid), or of fewer than k experts left, takes longer: a whole wave, one such token after the other.
  */
 enum { MOE_SCORE_SOFTMAX = 0, MOE_SCORE_SIGMOID = 1 };
 

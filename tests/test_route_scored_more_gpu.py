@@ -6,6 +6,7 @@ import torch
 
 import paper_2503_00245_amd as pkg
 from tests import operators_oracle as oo
+from tests.test_route_scored_gpu import CONFIGS, _config, _forward, _units
 
 pytestmark = pytest.mark.gpu
 
@@ -98,3 +99,96 @@ def test_gradients_of_experts_that_are_switched_off_play_no_part(E, k, sigmoid, 
         assert torch.isfinite(out[aux]).all()
         assert not out[aux][torch.from_numpy(dead).to(dev())].any()
         assert torch.equal(out[aux], out[2 + aux]) and torch.equal(out[aux], out[4 + aux])
+
+
+def _keys(l, bias, sigmoid):
+    return oo.scores(l[None], sigmoid)[0] + bias.astype(np.float64)
+
+
+def _ranks(key, groups):
+    return np.sort(key.reshape(groups, -1), axis=1)[:, -2:].sum(1)
+
+
+def _clear(rng, E, groups, kept, k, bias, sigmoid):
+    """Logits of a token whose picks, in their order, and whose groups are far from every other choice."""
+    while True:
+        l = (rng.standard_normal(E) * 1.5).astype(np.float32)
+        key = _keys(l, bias, sigmoid)
+        r = np.sort(_ranks(key, groups))[::-1]
+        if groups > 1 and r[kept - 1] - r[kept] < 2.0 ** -10:
+            continue
+        best = np.argsort(-_ranks(key, groups))[:kept]
+        left = np.sort(np.where(np.isin(np.arange(E) // (E // groups), best), key, -np.inf))[::-1]
+        if (left[:k] - left[1:k + 1]).min() > 2.0 ** -12:
+            return l
+
+
+def _near(l, e, gap):
+    """l with the logit of expert e where gap(l), which grows with it, is next to zero: more than sums in 64 bits are wrong by, less
+    than 32 bits can tell.  None: there is no such logit"""
+    l, lo, hi = l.astype(np.float64), -20.0, 20.0
+    for _ in range(80):
+        l[e] = (lo + hi) / 2
+        lo, hi = (l[e], hi) if gap(l) < 0 else (lo, l[e])
+    l = l.astype(np.float32)
+    return l if 2.0 ** -40 < abs(gap(l)) < 2.0 ** -23 else None
+
+
+NEAR = [(64, 8, 1, 1), (64, 8, 8, 4), (256, 8, 8, 4), (48, 3, 4, 2), (20, 4, 4, 3)]  # E, k, groups, kept
+
+
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("E,k,groups,kept,where", [(*c, "last pick") for c in NEAR] + [(*c, "group") for c in NEAR[1:]])
+def test_a_near_tie_in_one_place_of_one_token_of_four(E, k, groups, kept, where, sigmoid):
+    # a wave has four tokens: one of each four, in turn, has two keys at the last pick's border, or two ranks at the last group's, that 32 bits do not tell apart
+    print("near", E, k, groups, kept, sigmoid, where, flush=True)
+    rng = np.random.default_rng(E + groups)
+    bias = (rng.standard_normal(E) * 0.2).astype(np.float32)
+    per, rows, signs = E // groups, [], []
+    while len(rows) < 64:
+        l = _clear(rng, E, groups, kept, k, bias, sigmoid)
+        if len(rows) % 4 == len(rows) // 4 % 4:
+            key, rank = _keys(l, bias, sigmoid), _ranks(_keys(l, bias, sigmoid), groups)
+            order = np.argsort(-rank)
+            if where == "group":
+                inside, outside = order[kept - 1], order[kept]
+                e = outside * per + int(np.argmax(key[outside * per:(outside + 1) * per]))  # the best expert of the best group that is out
+
+                def gap(z):
+                    r = _ranks(_keys(z, bias, sigmoid), groups)
+                    return r[outside] - r[inside]
+            else:
+                left = np.argsort(-np.where(np.isin(np.arange(E) // per, order[:kept]), key, -np.inf))
+                a, e = left[k - 1], left[k]
+
+                def gap(z):
+                    c = _keys(z, bias, sigmoid)
+                    return c[e] - c[a]
+            l = _near(l, e, gap)
+            if l is None:
+                continue
+            signs.append(gap(l) > 0)
+        rows.append(l)
+    assert 0 < sum(signs) < len(signs) == 16
+    l = np.stack(rows)
+    c = (E, k, sigmoid, True, groups, kept, 2, True, 1.0)
+    ref, _, _ = oo.route(l, bias, k, sigmoid, groups, kept, 2, True, 1.0)
+    assert np.array_equal(_forward(c, l, bias)[0].cpu().numpy(), ref)
+
+
+@pytest.mark.parametrize("std", [6, 40])
+@pytest.mark.parametrize("c", [c for c in CONFIGS if c[3] or c[6] == 2])
+def test_spread_logits_are_picked_by_keys_in_64_bits(c, std):
+    # most scores are 0 or 1 to 32 bits, many to 64: those tie, and go by index (keys compared through logits, which do not, are not among these configurations)
+    print("spread", c, std, flush=True)
+    E, k, sigmoid, with_bias, groups, kept, top, renorm, scale = c
+    for T in (1, 67):
+        rng = np.random.default_rng(E * 3 + k + T + std)
+        l = (rng.standard_normal((T, E)) * std).astype(np.float32)
+        bias = (rng.standard_normal(E) * 0.3).astype(np.float32) if with_bias else None
+        idx, gate, s = _forward(c, l, bias)
+        ref_idx, ref_gate, ref_s = oo.route(l, np.zeros(E, np.float32) if bias is None else bias, k, sigmoid, groups, kept, top, renorm, scale)
+        assert np.array_equal(idx.cpu().numpy(), ref_idx)
+        u, tiny = _units(l, k, E), 2.0 ** -124
+        assert (np.abs(gate.double().cpu().numpy() - ref_gate) <= u * np.abs(ref_gate) + tiny * scale).all()
+        assert (np.abs(s.double().cpu().numpy() - ref_s) <= u * ref_s + tiny).all()
