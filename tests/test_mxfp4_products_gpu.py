@@ -63,3 +63,27 @@ def test_tiled_products(T, d, F, E, k, skew, hidden, down, dtype):
     # a row's sums are formed in the same order wherever it lies in a tile: copies of a token have its bits
     same = (y == y[:PATTERNS][pattern]).all(1)
     assert same.all(), same.logical_not().nonzero()[:8].flatten().tolist()
+
+
+@pytest.mark.parametrize("T,d,F,E,k,skew,hidden,down", [c for c in TILED if c[-2:] in ((128, 64), (128, 256), (256, 128), (64, 128))][:6])
+def test_a_token_of_nan_and_bad_picks_in_a_tile_leave_the_others_as_they_are(T, d, F, E, k, skew, hidden, down):
+    print("alone", T, d, F, E, k, hidden, down, flush=True)
+    rng = np.random.default_rng(T + F)
+    w, _ = _layer(rng, E, d, F)
+    weights = pkg.make_mxfp4_weights(w)
+    idx, gate = picks(E, k, skew)
+    pattern = torch.arange(T, device=dev()) % PATTERNS
+    i, g = torch.from_numpy(idx).to(dev())[pattern], torch.from_numpy(gate).to(dev())[pattern]
+    x = torch.from_numpy(rng.standard_normal((T, d)).astype(np.float32)).bfloat16().to(dev())
+    want = _run(x, w, i, g, E, k, d, F, "bf16", False, weights).clone()
+    odd = torch.tensor([0, 1, T // 3, T // 2, T - 1], device=dev())
+    others = torch.ones(T, dtype=torch.bool, device=dev())
+    others[odd] = False
+    x2, i2 = x.clone(), i.clone()
+    x2[odd, d - 1] = torch.tensor([float("nan"), float("inf"), -float("inf"), float("nan"), float("nan")], device=dev()).bfloat16()
+    y = _run(x2, w, i, g, E, k, d, F, "bf16", False, weights)
+    assert torch.equal(y[others], want[others])
+    assert torch.isnan(y[odd]).all()
+    i2[odd] = torch.tensor([-1, E, 1 << 30, -(1 << 31), E + 63], dtype=torch.int32, device=dev())[:, None]
+    y = _run(x, w, i2, g, E, k, d, F, "bf16", False, weights)
+    assert torch.equal(y[others], want[others])
