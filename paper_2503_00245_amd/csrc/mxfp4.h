@@ -20,7 +20,7 @@ constexpr int kMxCodes = 32 * kMxUnit / 2, kMxScales = 32 * kMxUnit / kMxBlock; 
 // instructions take by byte select.  Rows and columns are padded with zeros to whole units.
 // Activations (operand B, whose rows become the columns of the result): tile t holds rows 16 t ... of the block.
 // Weights (operand A): row m of tile t is row 8 (m / 4) + 4 t + m % 4 of the block, so that a lane's four results
-// of each of the two tiles are eight neighbours of an output row: one dword of codes or 16 bytes of bf16.
+// of each of the two tiles are eight neighbours of an output row: one dword of codes or 32 bytes of fp32.
 __host__ __device__ constexpr int mx_blocks(int rows) { return (rows + 31) / 32; }
 __host__ __device__ constexpr int mx_units(int cols) { return (cols + kMxUnit - 1) / kMxUnit; }
 
@@ -150,8 +150,9 @@ struct MxLayout {  // byte offsets of a workspace; every region starts 256-byte 
 MxLayout mx_layout(const moe_shape& s);
 int launch_mx_experts(const moe_shape& s, const moe_mxfp4_weights& w, const void* x, const int32_t* idx, const float* gate, void* y,
                       const MxLayout& l, char* ws, hipStream_t st);
-// Few pairs: two launches, without a dispatch (mxfp4_few.hip).  Whole layer, us, in these / in four launches: 2048 / 5632, 2 of 8 experts: one token
-// 14.7 / 20.3, two 20.4 / 23.9, four 35.3 / 37.0, eight 42.5 / 42.3; 1024 / 2816, 4 of 16 experts, four tokens 27.2 / 22.3.
+// Few pairs: two launches, without a dispatch (mxfp4_few.hip).  Whole layer, us, weights cold, in these / in four launches: 2048 / 5632, 2 of 8 experts:
+// one token 14.6 / 23.8, two 19.7 / 26.7, four 33.2 / 39.3; 1024 / 2816, 4 of 16 experts, two tokens 15.9 / 19.5.  With up to 16 pairs, eight tokens of the
+// former 42.2 / 42.7, four of the latter 24.7 / 22.0.
 constexpr int kMxFewPairs = 8;
 inline bool mx_few(const moe_shape& s) { return (long long)s.n_tokens * s.top_k <= kMxFewPairs; }
 int launch_mx_few(const moe_shape& s, const moe_mxfp4_weights& w, const void* x, const int32_t* idx, const float* gate, void* y, const MxLayout& l, char* ws,

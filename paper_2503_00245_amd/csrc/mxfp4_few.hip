@@ -63,7 +63,7 @@ __device__ __forceinline__ size_t row_scale(int p, int c, int q, int units) {
     return ((size_t)(p >> 5) * units + (c >> 1)) * kMxScales + (q * 16 + (p & 15)) * 4 + (c & 1) * 2 + (p >> 4 & 1);
 }
 
-constexpr int kHiddenWaves = 4;  // (of 2048 / 5632, us, with eight: two tokens 19.7 -> 19.4, four 35.6 -> 34.0)
+constexpr int kHiddenWaves = 4;  // (whole layer, us, with eight / with these: 2048 / 5632, one token 14.5 / 14.6, two 19.5 / 19.7, four 34.8 / 33.2; 1024 / 2816, two 17.5 / 15.9)
 
 template <typename T>
 __global__ __launch_bounds__(kHiddenWaves* kWave) void mx_few_hidden_kernel(ptr_arg a_idx, ptr_arg a_x, ptr_arg a_gate, ptr_arg a_up, int P, int E, int k, int d,

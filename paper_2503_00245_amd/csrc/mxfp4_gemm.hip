@@ -11,9 +11,11 @@
 // The eight waves are two groups, one wave of each on every SIMD, half a unit apart: while one multiplies out of
 // registers, the other reads the fragments of its next unit.  Group 1 fetches, between its products.
 // Measured on 2048 / 5632, Zipf loads, us (products of a wave for itself straight from memory / this): gate/up 105 / 72 and down 69 / 38 at 2048 tokens,
-// 699 / 440 and 500 / 205 at 16384 (3.5 PFLOP/s; a loop of these instructions on random operands and nothing else 7.1, the clock at 1.7 GHz
-// under the board's power limit).  The matrix units are busy 42 % of the clocks, at 2.05 GHz; a tile of 256 by 256 takes 3200 clocks a unit and 14000
-// beside them, of which 7000 are the activation's exponentials and reciprocals.
+// 699 / 440 and 500 / 205 at 16384 (a loop of these instructions on random operands and nothing else reaches 7.1 PFLOP/s, the clock at 1.7 GHz
+// under the board's power limit).  Down's figures, here and below, are of rows stored in bf16; in fp32, as now, it takes 42 and 236: 3.3 PFLOP/s over both products.
+// The matrix units are busy 42 % of gate/up's clocks and 37 % of down's, at 2.0-2.1 GHz, so that it is not the power limit that holds them: a
+// tile of 256 by 256 takes 3200 clocks a unit and 14000 beside them, of which 7000 are the activation's exponentials and reciprocals, with one workgroup
+// a CU and so nothing under them.
 // Measured and not adopted: tiles one after the other in a workgroup, the fills running on into the next (447 and 204, 477 with a wait behind the stores); fills by the
 // group that reads (486 and 237: they stand before the reads); four waves of 128 by 128 and 256 accumulators, two thirds of the fragment reads
 // but one wave to a SIMD (607 and 251); fills every second product, column tiles in blocks of one, two or eight: none.

@@ -12,7 +12,7 @@ namespace {
 
 constexpr int kWaves = 4;
 
-// ONCE: most experts have one group of rows, and the weights need not stay in the caches (2048 / 5632, 32 tokens 46.1 -> 43.7 us a layer)
+// ONCE: most experts have one group of rows, and the weights need not stay in the caches (2048 / 5632, 32 tokens 45.1 -> 42.3 us a layer, 1024 / 2816, 24 tokens 28.6 -> 27.3)
 template <bool SWIGLU, bool ONCE>
 __global__ __launch_bounds__(kWaves* kWave) void mx_stream_kernel(ptr_arg a_starts, ptr_arg a_w0, ptr_arg a_w1, ptr_arg a_rows, int E, int N, int K, int all_blocks,
                                                                   ptr_arg a_out) {
