@@ -1,5 +1,5 @@
-"""ctypes binding of libmoe_mi355x.so: the entry points of include/moe.h and
-include/moe_quantised.h under the same names.
+"""ctypes binding of libmoe_mi355x.so: the entry points of include/moe.h,
+include/moe_quantised.h and include/moe_training.h under the same names.
 
 Argument marshalling only: tensors are torch CUDA(HIP) tensors used for device memory
 and the current stream; every step of the layer runs in the library's kernels.  There
@@ -27,6 +27,9 @@ EXPORTS = ("moe_route", "moe_permute", "moe_expert_ffn", "moe_combine", "moe_for
 QUANTISED_EXPORTS = ("moe_route_scored", "moe_route_scored_backward", "moe_mxfp4_quantize", "moe_mxfp4_dequantize",
                      "moe_mxfp4_packed_bytes", "moe_mxfp4_pack", "moe_mxfp4_workspace_bytes", "moe_mxfp4_experts",
                      "moe_mxfp4_forward")  # include/moe_quantised.h
+TRAINING_EXPORTS = ("moe_training_workspace_bytes", "moe_dispatch", "moe_dispatch_backward", "moe_collect", "moe_collect_backward",
+                    "moe_expert_ffn_backward", "moe_block_norm", "moe_block_workspace_bytes", "moe_block_norm_backward",
+                    "moe_block_stack_workspace_bytes", "moe_block_stack_forward")  # include/moe_training.h
 
 
 class MoeShape(C.Structure):
@@ -48,6 +51,11 @@ class RouteConfig(C.Structure):
 
 class Mxfp4WeightsStruct(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("router_w", "router_b", "select_bias", "gate", "up", "down")]
+
+
+class BlockStruct(C.Structure):
+    _fields_ = [(n, C.c_float) for n in ("eps", "skip_scale", "block_scale", "dropout")] + \
+               [(n, C.c_void_p) for n in ("post_w", "gate", "token_gate", "rng")]
 
 
 class MoeError(RuntimeError):
@@ -102,6 +110,23 @@ def lib() -> C.CDLL:
         L.moe_mxfp4_workspace_bytes.restype = sz
         L.moe_mxfp4_experts.argtypes = [sp, qp, vp, vp, vp, vp, vp, sz, vp]
         L.moe_mxfp4_forward.argtypes = [sp, rp, qp, vp, vp, vp, vp, vp, vp, sz, vp]
+        bp = C.POINTER(BlockStruct)
+        L.moe_training_workspace_bytes.argtypes = [sp]
+        L.moe_block_workspace_bytes.argtypes = [i32, i32]
+        L.moe_block_stack_workspace_bytes.argtypes = [sp]
+        for fn in ("moe_training_workspace_bytes", "moe_block_workspace_bytes", "moe_block_stack_workspace_bytes"):
+            getattr(L, fn).restype = sz
+        L.moe_dispatch.argtypes = [sp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.moe_dispatch_backward.argtypes = [sp, vp, vp, vp, vp, vp, vp, vp]
+        L.moe_collect.argtypes = [sp, vp, vp, vp, vp, vp, vp]
+        L.moe_collect_backward.argtypes = [sp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.moe_expert_ffn_backward.argtypes = [sp, wp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.moe_block_norm.argtypes = [bp, i32, i32, i32, vp, vp, vp, vp, vp, vp]
+        L.moe_block_norm_backward.argtypes = [bp, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.moe_block_stack_forward.argtypes = [sp, wp, bp, C.POINTER(vp), i32, vp, vp, vp, vp, sz, vp]
+        for fn in ("moe_dispatch", "moe_dispatch_backward", "moe_collect", "moe_collect_backward", "moe_expert_ffn_backward", "moe_block_norm",
+                   "moe_block_norm_backward", "moe_block_stack_forward"):
+            getattr(L, fn).restype = C.c_int
         for fn in ("moe_route_scored", "moe_route_scored_backward", "moe_mxfp4_quantize", "moe_mxfp4_dequantize",
                    "moe_mxfp4_pack", "moe_mxfp4_experts", "moe_mxfp4_forward"):
             getattr(L, fn).restype = C.c_int
@@ -460,3 +485,187 @@ def moe_mxfp4_forward(shape: MoeShape, config: RouteConfig, weights: Mxfp4Weight
     pl = _arg("logits", logits, torch.float32, (shape.n_tokens, shape.n_experts), x.get_device())
     _check("moe_mxfp4_forward", lib().moe_mxfp4_forward(C.byref(shape), C.byref(config), C.byref(weights.struct), px, py, pi, pg, pl,
                                                         pw, n, _stream(x.device)))
+
+
+# ---- a training step around and through the experts --------------------------------------------------------------
+
+def moe_training_workspace_bytes(shape: MoeShape) -> int:
+    return int(lib().moe_training_workspace_bytes(C.byref(shape)))
+
+
+def alloc_training_workspace(shape: MoeShape, device) -> torch.Tensor:
+    n = moe_training_workspace_bytes(shape)
+    if n == 0 and shape.n_tokens > 0:
+        raise MoeError("moe_training_workspace_bytes", -1)
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _bytes(workspace: Optional[torch.Tensor]) -> int:
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def _workspace(workspace: Optional[torch.Tensor], device: int):
+    if workspace is not None and workspace.get_device() != device:
+        raise ValueError("workspace on another device than the call's first tensor")
+    return _ptr(workspace)
+
+
+def _layer_sizes(shape: MoeShape):
+    """Shapes of tokens, rows, picks and pairs, and the type of rows"""
+    T, d, k = shape.n_tokens, shape.d_model, shape.top_k
+    return (T, d), (T * k, d), (T, k), (T * k,), _DTYPES.get(shape.act_dtype)
+
+
+def _pairs_arg(name: str, t, dtype, shape: MoeShape, device: int):
+    """Pointer of a value for each pair, [T,k] or [T k]"""
+    picks, pairs = (shape.n_tokens, shape.top_k), (shape.n_tokens * shape.top_k,)
+    return _arg(name, t, dtype, pairs if t is not None and t.dim() == 1 else picks, device)
+
+
+def moe_dispatch(shape: MoeShape, topk_idx, weight, x, expert_offsets, perm, inv_perm, x_perm, workspace=None) -> None:
+    """topk_idx int32 [T,k], weight f32 [T,k] or None, x [T,d]; expert_offsets int32 [E+1], perm and inv_perm int32 [T k],
+    x_perm [T k,d]: outputs."""
+    tokens, rows, picks, pairs, dtype = _layer_sizes(shape)
+    at, i32 = x.get_device(), torch.int32
+    _check("moe_dispatch", lib().moe_dispatch(
+        C.byref(shape), _arg("topk_idx", topk_idx, i32, picks, at), _arg("weight", weight, torch.float32, picks, at), _arg("x", x, dtype, tokens, at),
+        _arg("expert_offsets", expert_offsets, i32, (shape.n_experts + 1,), at), _arg("perm", perm, i32, pairs, at),
+        _pairs_arg("inv_perm", inv_perm, i32, shape, at), _arg("x_perm", x_perm, dtype, rows, at), _workspace(workspace, at), _bytes(workspace),
+        _stream(x.device)))
+
+
+def moe_dispatch_backward(shape: MoeShape, grad_x_perm, inv_perm, x, weight, grad_x, grad_weight=None) -> None:
+    """grad_x_perm [T k,d], inv_perm int32 [T k] or [T,k], x [T,d] or None without grad_weight, weight f32 [T,k] or None; grad_x [T,d]
+    and grad_weight f32 [T,k] (or None): outputs."""
+    tokens, rows, picks, _, dtype = _layer_sizes(shape)
+    at, f32 = grad_x_perm.get_device(), torch.float32
+    _check("moe_dispatch_backward", lib().moe_dispatch_backward(
+        C.byref(shape), _arg("grad_x_perm", grad_x_perm, dtype, rows, at), _pairs_arg("inv_perm", inv_perm, torch.int32, shape, at),
+        _arg("x", x, dtype, tokens, at), _arg("weight", weight, f32, picks, at), _arg("grad_x", grad_x, dtype, tokens, at),
+        _arg("grad_weight", grad_weight, f32, picks, at), _stream(grad_x_perm.device)))
+
+
+def moe_collect(shape: MoeShape, y_perm, inv_perm, topk_gate, residual, y) -> None:
+    """y_perm [T k,d], inv_perm int32 [T k] or [T,k], topk_gate f32 [T,k], residual [T,d] or None; y [T,d]: output."""
+    tokens, rows, picks, _, dtype = _layer_sizes(shape)
+    at = y_perm.get_device()
+    _check("moe_collect", lib().moe_collect(
+        C.byref(shape), _arg("y_perm", y_perm, dtype, rows, at), _pairs_arg("inv_perm", inv_perm, torch.int32, shape, at),
+        _arg("topk_gate", topk_gate, torch.float32, picks, at), _arg("residual", residual, dtype, tokens, at), _arg("y", y, dtype, tokens, at),
+        _stream(y_perm.device)))
+
+
+def moe_collect_backward(shape: MoeShape, grad_y, y_perm, expert_offsets, inv_perm, topk_gate, grad_y_perm=None, grad_gate=None) -> None:
+    """grad_y [T,d], y_perm [T k,d] or None without grad_gate, expert_offsets int32 [E+1], inv_perm int32 [T k] or [T,k], topk_gate
+    f32 [T,k]; grad_y_perm [T k,d] and grad_gate f32 [T,k], either or None: outputs."""
+    tokens, rows, picks, _, dtype = _layer_sizes(shape)
+    at, f32 = grad_y.get_device(), torch.float32
+    _check("moe_collect_backward", lib().moe_collect_backward(
+        C.byref(shape), _arg("grad_y", grad_y, dtype, tokens, at), _arg("y_perm", y_perm, dtype, rows, at),
+        _arg("expert_offsets", expert_offsets, torch.int32, (shape.n_experts + 1,), at), _pairs_arg("inv_perm", inv_perm, torch.int32, shape, at),
+        _arg("topk_gate", topk_gate, f32, picks, at), _arg("grad_y_perm", grad_y_perm, dtype, rows, at),
+        _arg("grad_gate", grad_gate, f32, picks, at), _stream(grad_y.device)))
+
+
+def moe_expert_ffn_backward(shape: MoeShape, weights: MoeWeights, x_perm, expert_offsets, grad_y_perm, grad_x_perm=None, grad_w_gate=None,
+                            grad_w_up=None, grad_w_down=None, workspace=None) -> None:
+    """x_perm, grad_y_perm [T k,d], expert_offsets int32 [E+1]; grad_x_perm [T k,d], grad_w_gate and grad_w_up [E,F,d], grad_w_down
+    [E,d,F], each of them or None: outputs."""
+    _, rows, _, _, dtype = _layer_sizes(shape)
+    E, d, F, at = shape.n_experts, shape.d_model, shape.d_ff, x_perm.get_device()
+    _check("moe_expert_ffn_backward", lib().moe_expert_ffn_backward(
+        C.byref(shape), C.byref(weights), _arg("x_perm", x_perm, dtype, rows, at), _arg("expert_offsets", expert_offsets, torch.int32, (E + 1,), at),
+        _arg("grad_y_perm", grad_y_perm, dtype, rows, at), _arg("grad_x_perm", grad_x_perm, dtype, rows, at),
+        _arg("grad_w_gate", grad_w_gate, dtype, (E, F, d), at), _arg("grad_w_up", grad_w_up, dtype, (E, F, d), at),
+        _arg("grad_w_down", grad_w_down, dtype, (E, d, F), at), _workspace(workspace, at), _bytes(workspace), _stream(x_perm.device)))
+
+
+class Block:
+    """What stands at the end of a block: its numbers, and the tensors that hold its weights."""
+
+    def __init__(self, struct: BlockStruct, tensors: Dict[str, Optional[torch.Tensor]]):
+        self.struct, self.tensors = struct, tensors
+
+
+def make_block(eps=1e-5, skip_scale=1.0, block_scale=1.0, dropout=0.0, post_w=None, gate=None, token_gate=None, rng=None) -> Block:
+    """post_w, gate f32 [d], token_gate f32 [T], each or None; rng int64 or uint64 [2] (seed, offset) on the device, needed for dropout."""
+    t = {"post_w": post_w, "gate": gate, "token_gate": token_gate, "rng": rng}
+    for name in ("post_w", "gate", "token_gate"):
+        if t[name] is not None:
+            _want(name, t[name], torch.float32, t[name].numel())
+    if rng is not None and (rng.dtype not in (torch.int64, torch.uint64) or rng.shape != (2,)):
+        raise ValueError(f"rng must be two int64 or uint64 values, got {rng.dtype} {list(rng.shape)}")
+    return Block(BlockStruct(eps, skip_scale, block_scale, dropout, *(_ptr(v) for v in t.values())), t)
+
+
+def moe_block_workspace_bytes(n_tokens: int, d_model: int) -> int:
+    return int(lib().moe_block_workspace_bytes(n_tokens, d_model))
+
+
+def alloc_block_workspace(n_tokens: int, d_model: int, device) -> torch.Tensor:
+    n = moe_block_workspace_bytes(n_tokens, d_model)
+    if n == 0:
+        raise MoeError("moe_block_workspace_bytes", -1)
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _block_check(block: Block, T: int, d: int, device: int, weights: bool) -> None:
+    for name, n in (("post_w", d), ("gate", d), ("token_gate", T)) if weights else ():
+        v = block.tensors[name]
+        if v is not None and v.shape[0] != n:
+            raise ValueError(f"{name} must have {n} values, got {v.shape[0]}")
+    for v in block.tensors.values():
+        if v is not None and v.get_device() != device:
+            raise ValueError("the block's tensors on another device than the call's first tensor")
+
+
+def moe_block_norm(block: Block, x, b, open_w, y, n) -> None:
+    """x, b [T,d], open_w f32 [d]; y and n [T,d]: outputs.  open_w and n, or b and y, may be None together."""
+    T, d = rows = x.shape
+    at, dtype = x.get_device(), x.dtype
+    _block_check(block, T, d, at, b is not None)
+    _check("moe_block_norm", lib().moe_block_norm(
+        C.byref(block.struct), T, d, _act_dtype(x), _arg("x", x, dtype, rows, at), _arg("b", b, dtype, rows, at),
+        _arg("open_w", open_w, torch.float32, (d,), at), _arg("y", y, dtype, rows, at), _arg("n", n, dtype, rows, at), _stream(x.device)))
+
+
+def moe_block_norm_backward(block: Block, grad_y, grad_n, y, b, open_w, grad_x, grad_b=None, grad_open_w=None, grad_post_w=None, grad_gate=None,
+                            grad_token_gate=None, workspace=None) -> None:
+    """grad_y, grad_n, y, b [T,d], open_w f32 [d], as they apply; grad_x, grad_b [T,d], grad_open_w, grad_post_w, grad_gate f32 [d],
+    grad_token_gate f32 [T], each of the last four or None: outputs."""
+    T, d = rows = grad_x.shape
+    at, dtype, f32 = grad_x.get_device(), grad_x.dtype, torch.float32
+    _block_check(block, T, d, at, b is not None)
+    _check("moe_block_norm_backward", lib().moe_block_norm_backward(
+        C.byref(block.struct), T, d, _act_dtype(grad_x), _arg("grad_y", grad_y, dtype, rows, at), _arg("grad_n", grad_n, dtype, rows, at),
+        _arg("y", y, dtype, rows, at), _arg("b", b, dtype, rows, at), _arg("open_w", open_w, f32, (d,), at), _arg("grad_x", grad_x, dtype, rows, at),
+        _arg("grad_b", grad_b, dtype, rows, at), _arg("grad_open_w", grad_open_w, f32, (d,), at), _arg("grad_post_w", grad_post_w, f32, (d,), at),
+        _arg("grad_gate", grad_gate, f32, (d,), at), _arg("grad_token_gate", grad_token_gate, f32, (T,), at), _workspace(workspace, at),
+        _bytes(workspace), _stream(grad_x.device)))
+
+
+def moe_block_stack_workspace_bytes(shape: MoeShape) -> int:
+    return int(lib().moe_block_stack_workspace_bytes(C.byref(shape)))
+
+
+def alloc_block_stack_workspace(shape: MoeShape, device) -> torch.Tensor:
+    n = moe_block_stack_workspace_bytes(shape)
+    if n == 0:
+        raise MoeError("moe_block_stack_workspace_bytes", -1)
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def moe_block_stack_forward(shape: MoeShape, layers: Sequence[MoeWeights], blocks: Sequence[Block], open_w: Sequence[torch.Tensor], x, y,
+                            topk_trace=None, workspace=None) -> None:
+    """x [T,d], for each layer its weights, its block and open_w f32 [d]; y [T,d] and topk_trace int32 [L,T,k] (or None): outputs."""
+    n, T, d = len(layers), shape.n_tokens, shape.d_model
+    if len(blocks) != n or len(open_w) != n:
+        raise ValueError(f"{n} layers, {len(blocks)} blocks and {len(open_w)} norms")
+    at, dtype = x.get_device(), _DTYPES.get(shape.act_dtype)
+    for block in blocks:
+        _block_check(block, T, d, at, True)
+    _check("moe_block_stack_forward", lib().moe_block_stack_forward(
+        C.byref(shape), (MoeWeights * n)(*layers), (BlockStruct * n)(*(b.struct for b in blocks)),
+        (C.c_void_p * n)(*(_arg("open_w", w, torch.float32, (d,), at) for w in open_w)), n, _arg("x", x, dtype, (T, d), at),
+        _arg("y", y, dtype, (T, d), at), _arg("topk_trace", topk_trace, torch.int32, (n, T, shape.top_k), at), _workspace(workspace, at),
+        _bytes(workspace), _stream(x.device)))

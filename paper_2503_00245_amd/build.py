@@ -14,7 +14,8 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libmoe_mi355x.so")
 SOURCES = ["api.hip", "route.hip", "permute.hip", "combine.hip", "expert_gemv.hip", "expert_gemv_one.hip", "expert_gemm.hip", "expert_gemm_f32.hip",
            "expert_gemm_pp.hip", "expert_gemm_few.hip",
-           "metrics.hip", "route_scored.hip", "mxfp4_rows.hip", "mxfp4_experts.hip", "mxfp4_few.hip", "mxfp4_gemm.hip", "mxfp4_stream.hip"]
+           "metrics.hip", "route_scored.hip", "mxfp4_rows.hip", "mxfp4_experts.hip", "mxfp4_few.hip", "mxfp4_gemm.hip", "mxfp4_stream.hip",
+           "dispatch_rows.hip", "block_norm.hip", "expert_grad.hip", "expert_grad_mfma.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          # scalar arguments at the head of a kernel's list arrive in registers instead of by a load: 0.2-0.5 us a launch

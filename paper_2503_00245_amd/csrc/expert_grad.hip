@@ -1,0 +1,260 @@
+// Gradient of the experts (moe_training.h states it): the order of its products, and kernels for any type and size.
+//
+// Three launches: a, b and dh with the activation's gradient behind them, then the gradients of the weights and of the rows.
+// The forward pass keeps nothing for it: a and b are formed again (4 of 16 P d F operations), which is less than what reading
+// them back would save in any program that holds more than a few layers' worth of rows.
+//
+// The kernels here: tiles of 64 x 64 on four waves, operands widened to fp32 in LDS, v_mfma_f32_16x16x4_f32.
+#include "expert_grad.h"
+
+namespace moe {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int TILE = 64, STEP = 16, PITCH = TILE + 4;
+
+// A tile's share of one operand: 16 k by 64 rows (or columns) in fp32, [k][row].  K_CONTIGUOUS: memory holds [row][k].
+template <typename T, bool K_CONTIGUOUS>
+struct Operand {
+    const T* base;       // of the expert's matrix or the group's first row
+    long long pitch;     // elements from one row of memory to the next
+    int rows, K;         // valid rows (columns) from `first` on, valid k
+    int first;
+
+    __device__ __forceinline__ f32x4 load(int k0) const {
+        const int t = threadIdx.x;
+        const T* p;
+        bool ok;
+        if (K_CONTIGUOUS) {  // four k of a row
+            const int r = t >> 2, k = k0 + (t & 3) * 4;
+            ok = r < rows && k < K;
+            p = base + (first + r) * pitch + k;
+        } else {             // four rows of a k
+            const int r = (t & 15) * 4, k = k0 + (t >> 4);
+            ok = r < rows && k < K;
+            p = base + k * pitch + first + r;
+        }
+        f32x4 v{0.f, 0.f, 0.f, 0.f};
+        if (ok) {
+            if constexpr (sizeof(T) == 4) {
+                v = *reinterpret_cast<const f32x4*>(p);
+            } else {
+                const bf16x4 b = *reinterpret_cast<const bf16x4*>(p);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = (float)b[i];
+            }
+        }
+        return v;
+    }
+    __device__ __forceinline__ void store(float (*s)[PITCH], const f32x4& v) const {
+        const int t = threadIdx.x;
+        if (K_CONTIGUOUS) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[(t & 3) * 4 + i][t >> 2] = v[i];
+        } else {
+            *reinterpret_cast<f32x4*>(&s[t >> 4][(t & 15) * 4]) = v;
+        }
+    }
+};
+
+struct Tile {
+    float a[STEP][PITCH], b[STEP][PITCH];
+};
+
+// acc[i][j] += the products of 16-row block i and 16-column block j of the wave's 32 x 32; a lane's four values are neighbouring
+// columns of one row
+template <typename OA, typename OB>
+__device__ __forceinline__ void multiply(Tile& s, const OA& a, const OB& b, int K, f32x4 (&acc)[2][2]) {
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const int m0 = (wave >> 1) * 32 + (lane & 15), n0 = (wave & 1) * 32 + (lane & 15);
+    f32x4 va = a.load(0), vb = b.load(0);
+    for (int k0 = 0; k0 < K; k0 += STEP) {
+        __syncthreads();
+        a.store(s.a, va);
+        b.store(s.b, vb);
+        __syncthreads();
+        if (k0 + STEP < K) va = a.load(k0 + STEP), vb = b.load(k0 + STEP);
+#pragma unroll
+        for (int k = 0; k < STEP; k += 4) {
+            const int kk = k + (lane >> 4);
+            const float a0 = s.a[kk][m0], a1 = s.a[kk][m0 + 16], b0 = s.b[kk][n0], b1 = s.b[kk][n0 + 16];
+            acc[0][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(b0, a0, acc[0][0], 0, 0, 0);
+            acc[0][1] = __builtin_amdgcn_mfma_f32_16x16x4f32(b1, a0, acc[0][1], 0, 0, 0);
+            acc[1][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(b0, a1, acc[1][0], 0, 0, 0);
+            acc[1][1] = __builtin_amdgcn_mfma_f32_16x16x4f32(b1, a1, acc[1][1], 0, 0, 0);
+        }
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void put4(T* p, const f32x4& v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = Store<T>::from_f32(v[i]);
+}
+
+template <typename T, int OP>
+__global__ __launch_bounds__(kThreads) void grad_rows_kernel(const GradArgs g) {
+    __shared__ Tile s;
+    const int K = OP == GRAD_DX ? g.F : g.d, N = OP == GRAD_DX ? g.d : g.F;
+    int lo, hi, e, row0, row_end, nt;
+    group_bounds(g.offsets, g.E, g.P, lo, hi);
+    lo = min(max(lo, 0), g.P), hi = min(max(hi, lo), g.P);
+    if (!find_tile(lo, hi, g.E, TILE, [&](int) { return (N + TILE - 1) / TILE; }, e, row0, row_end, nt)) return;
+    const int n0 = nt * TILE;
+    const size_t at_w = (size_t)e * g.d * g.F;
+    const int rows = min(TILE, row_end - row0), cols = min(TILE, N - n0);
+    f32x4 acc[2][2] = {}, up[2][2] = {}, dh[2][2] = {};
+    if (OP == GRAD_ACT) {
+        const Operand<T, true> a{static_cast<const T*>(g.x), g.d, rows, K, row0};
+        const Operand<T, true> b{static_cast<const T*>(g.w_gate) + at_w, g.d, cols, K, n0}, b1{static_cast<const T*>(g.w_up) + at_w, g.d, cols, K, n0};
+        multiply(s, a, b, K, acc);
+        multiply(s, a, b1, K, up);
+        const Operand<T, true> a2{static_cast<const T*>(g.gy), g.d, rows, K, row0};
+        const Operand<T, false> b2{static_cast<const T*>(g.w_down) + at_w, g.F, cols, K, n0};
+        multiply(s, a2, b2, K, dh);
+    } else {
+        const Operand<T, true> a{static_cast<const T*>(g.da), g.F, rows, K, row0}, a1{static_cast<const T*>(g.db), g.F, rows, K, row0};
+        const Operand<T, false> b{static_cast<const T*>(g.w_gate) + at_w, g.d, cols, K, n0}, b1{static_cast<const T*>(g.w_up) + at_w, g.d, cols, K, n0};
+        multiply(s, a, b, K, acc);
+        multiply(s, a1, b1, K, acc);
+    }
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int r = (wave >> 1) * 32 + i * 16 + (lane & 15), c = (wave & 1) * 32 + j * 16 + (lane >> 4) * 4;
+            if (r >= rows || c >= cols) continue;
+            const size_t at = (size_t)(row0 + r) * N + n0 + c;
+            if (OP == GRAD_ACT) {
+                f32x4 h, da, db;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const ActGrad v = act_grad(acc[i][j][q], up[i][j][q], dh[i][j][q]);
+                    h[q] = v.h, da[q] = v.da, db[q] = v.db;
+                }
+                put4(static_cast<T*>(g.da) + at, da);
+                put4(static_cast<T*>(g.db) + at, db);
+                put4(static_cast<T*>(g.h) + at, h);
+            } else {
+                put4(static_cast<T*>(g.gx) + at, acc[i][j]);
+            }
+        }
+}
+
+// blockIdx.y: expert, z: which of the three gradients
+template <typename T>
+__global__ __launch_bounds__(kThreads) void grad_weights_kernel(const GradArgs g) {
+    __shared__ Tile s;
+    const int e = blockIdx.y, which = blockIdx.z;
+    const int M = which == 2 ? g.d : g.F, N = which == 2 ? g.F : g.d;
+    T* const out = static_cast<T*>(which == 0 ? g.gw_gate : which == 1 ? g.gw_up : g.gw_down);
+    if (!out) return;
+    const int mt_all = (M + TILE - 1) / TILE, nt = quick_div(blockIdx.x, mt_all), mt = blockIdx.x - nt * mt_all;
+    const int m0 = mt * TILE, n0 = nt * TILE;
+    if (n0 >= N) return;
+    const int lo = g.P ? min(max(g.offsets[e], 0), g.P) : 0, hi = g.P ? min(max(g.offsets[e + 1], lo), g.P) : 0;
+    const int rows = min(TILE, M - m0), cols = min(TILE, N - n0), K = hi - lo;
+    f32x4 acc[2][2] = {};
+    if (K > 0) {
+        const T* const left = static_cast<const T*>(which == 0 ? g.da : which == 1 ? g.db : g.gy) + (size_t)lo * M;
+        const T* const right = static_cast<const T*>(which == 2 ? g.h : g.x) + (size_t)lo * N;
+        const Operand<T, false> a{left, M, rows, K, m0}, b{right, N, cols, K, n0};
+        multiply(s, a, b, K, acc);
+    }
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int r = (wave >> 1) * 32 + i * 16 + (lane & 15), c = (wave & 1) * 32 + j * 16 + (lane >> 4) * 4;
+            if (r < rows && c < cols) put4(out + (size_t)e * M * N + (size_t)(m0 + r) * N + n0 + c, acc[i][j]);
+        }
+}
+
+template <typename T>
+int run_plain(const GradArgs& g, GradOp op, hipStream_t st) {
+    if (op == GRAD_WEIGHTS) {
+        const unsigned tiles = (unsigned)((g.d + TILE - 1) / TILE) * ((g.F + TILE - 1) / TILE);
+        hipLaunchKernelGGL(grad_weights_kernel<T>, dim3(tiles, g.E, 3), dim3(kThreads), 0, st, g);
+        return launch_status();
+    }
+    const int N = op == GRAD_DX ? g.d : g.F;
+    const int grid = find_tile_grid(m_tiles_bound(g.P, g.E, TILE) * ((N + TILE - 1) / TILE), 0);
+    const auto kern = op == GRAD_ACT ? grad_rows_kernel<T, GRAD_ACT> : grad_rows_kernel<T, GRAD_DX>;
+    hipLaunchKernelGGL(kern, dim3(grid), dim3(kThreads), 0, st, g);
+    return launch_status();
+}
+
+struct GradLayout {
+    size_t da, db, h, total;
+};
+GradLayout grad_layout(const moe_shape& s) {
+    const size_t hidden = round_up((size_t)s.n_tokens * s.top_k * s.d_ff * elt_size(s.act_dtype), 256);
+    return GradLayout{0, hidden, 2 * hidden, 3 * hidden};
+}
+
+int validate_grad(const moe_shape* s) {
+    const int rc = validate_shape(s);
+    if (rc != MOE_OK) return rc;
+    // tiles of a launch are counted in 31 bits
+    const long long tiles_d = (s->d_model + TILE - 1) / TILE, tiles_f = (s->d_ff + TILE - 1) / TILE;
+    const long long rows = ((long long)s->n_tokens * s->top_k + TILE - 1) / TILE + s->n_experts;
+    if (s->rank != 0 || s->d_model > (1 << 18) || s->d_ff > (1 << 18) || tiles_d * tiles_f >= (1 << 23) || rows * (tiles_d > tiles_f ? tiles_d : tiles_f) >= (1 << 23))
+        return MOE_ERR_UNSUPPORTED;
+    return MOE_OK;
+}
+
+}  // namespace
+
+size_t dispatch_scratch_bytes(long long T, int E);  // dispatch_rows.hip
+
+int run_grad_plain(const GradArgs& g, GradOp op, int act_dtype, hipStream_t st) {
+    return act_dtype == MOE_F32 ? run_plain<float>(g, op, st) : run_plain<bf16_t>(g, op, st);
+}
+
+}  // namespace moe
+
+using namespace moe;
+
+extern "C" size_t moe_training_workspace_bytes(const moe_shape* shape) {
+    if (validate_grad(shape) != MOE_OK) return 0;
+    const size_t sort = round_up(dispatch_scratch_bytes(shape->n_tokens, shape->n_experts), 256), grad = grad_layout(*shape).total;
+    return sort > grad ? sort : grad;
+}
+
+extern "C" int moe_expert_ffn_backward(const moe_shape* shape, const moe_weights* weights, const void* x_perm, const int32_t* expert_offsets,
+                                       const void* grad_y_perm, void* grad_x_perm, void* grad_w_gate, void* grad_w_up, void* grad_w_down,
+                                       void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = validate_grad(shape);
+    if (rc != MOE_OK) return rc;
+    const moe_shape& s = *shape;
+    const bool any_w = grad_w_gate || grad_w_up || grad_w_down;
+    for (const void* p : {(const void*)grad_x_perm, (const void*)grad_w_gate, (const void*)grad_w_up, (const void*)grad_w_down})
+        if (!aligned16(p) || (p && (p == x_perm || p == grad_y_perm))) return MOE_ERR_INVALID;
+    GradArgs g{};
+    g.P = s.n_tokens * s.top_k, g.E = s.n_experts, g.d = s.d_model, g.F = s.d_ff;
+    g.gx = grad_x_perm, g.gw_gate = grad_w_gate, g.gw_up = grad_w_up, g.gw_down = grad_w_down;
+    hipStream_t st = as_stream(stream);
+    if (g.P == 0) return any_w ? run_grad_plain(g, GRAD_WEIGHTS, s.act_dtype, st) : MOE_OK;
+    if (!weights || !x_perm || !grad_y_perm || !expert_offsets) return MOE_ERR_INVALID;
+    for (const void* p : {weights->w_gate, weights->w_up, weights->w_down})
+        if (!p) return MOE_ERR_INVALID;
+    for (const void* p : {weights->w_gate, weights->w_up, weights->w_down, x_perm, grad_y_perm})
+        if (!aligned16(p)) return MOE_ERR_INVALID;
+    if (reinterpret_cast<uintptr_t>(expert_offsets) & 3u) return MOE_ERR_INVALID;
+    const GradLayout l = grad_layout(s);
+    if (!workspace || workspace_bytes < l.total) return MOE_ERR_WORKSPACE;
+    if (!aligned16(workspace)) return MOE_ERR_INVALID;
+    if (!any_w && !grad_x_perm) return MOE_OK;
+    char* const ws = static_cast<char*>(workspace);
+    g.x = x_perm, g.gy = grad_y_perm, g.w_gate = weights->w_gate, g.w_up = weights->w_up, g.w_down = weights->w_down;
+    g.da = ws + l.da, g.db = ws + l.db, g.h = ws + l.h, g.offsets = expert_offsets;
+    const bool mfma = s.act_dtype == MOE_BF16 && grad_mfma_supported(g);
+    auto run = [&](GradOp op) { return mfma ? run_grad_mfma(g, op, st) : run_grad_plain(g, op, s.act_dtype, st); };
+    rc = run(GRAD_ACT);
+    if (rc == MOE_OK && any_w) rc = run(GRAD_WEIGHTS);
+    if (rc == MOE_OK && grad_x_perm) rc = run(GRAD_DX);
+    return rc;
+}

@@ -1,0 +1,428 @@
+// Gradient of bf16 experts on tiles of 256 rows, operands fetched from memory straight into LDS (expert_grad.h names the
+// products).
+//
+// What bounds it: matrix operations for many rows (16 P d F of them), weights and their gradients for few.
+//
+// Layouts.  An operand whose k-values are neighbours in memory (rows of x, gy, da, db; W_gate and W_up where k runs along
+// d) lies in LDS as rows of 128 bytes, a k-step, and a lane's eight k-values are one 16-byte read.  The other operands (W_down under dh,
+// W_gate and W_up under gx, and both operands of the gradients of weights, where k runs along the tokens) lie as they come,
+// 64 rows of k by the tile's columns, and are transposed on their way out of LDS: ds_read_b64_tr_b16 hands a lane four k-values of its
+// column, from four rows of which each of 16 lanes names 8 bytes.  No transposed copy of anything is made.  Both kinds of rows are swizzled
+// on the memory side so that reads meet no bank conflict: chunks of 16 bytes by half the row's number, and, in rows read transposed,
+// units of 32 bytes (16 columns) by bits 0, 1 and 3 of the row's (two groups of 16 lanes read rows r .. r + 3 and r + 8 .. r + 11).
+//
+// Schedule: that of expert_gemm_pp.hip.  Eight waves in two groups half a k-step apart: one multiplies out of registers while the
+// other reads the fragments of its whole next step; fills go between the products, B by group 0, A by group 1.
+//
+// The activation's gradient needs a, b and dh of the same place: one workgroup forms all three for 96 columns (144
+// accumulator registers a lane, 80 for a step's fragments), a and b in a first pass over d, dh in a second one.  dh then is never rounded nor
+// stored: as a tensor of its own in bf16 it raised the error of the gradients from 2.4e-3 to 2.9e-3.
+#include "expert_grad.h"
+#include "lds_fill.h"
+
+#include <algorithm>
+
+namespace moe {
+
+namespace {
+
+#define INLINE __attribute__((always_inline))
+
+constexpr int BM = 256, BK = 64, kThreads = 512;
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+// Four k-values of the lane's column, twice: rows at and at + rows4 of LDS
+__device__ __forceinline__ bf16x8 read_transposed(unsigned at, unsigned rows4) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4*>((uintptr_t)at));
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4*>((uintptr_t)(at + rows4)));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+#else
+    return bf16x8{};
+#endif
+}
+
+template <int OP>
+struct Form {
+    static constexpr bool ACT = OP == GRAD_ACT, WGT = OP == GRAD_WEIGHTS;
+    static constexpr int WAVES_M = ACT ? 4 : 2, WAVES_N = 8 / WAVES_M;
+    static constexpr int MB = 8 / WAVES_M;           // 32-row blocks of a wave: wm, wm + WAVES_M, ...
+    static constexpr int BN = ACT ? 96 : 256;        // output columns
+    static constexpr int NI = ACT ? 6 : 4;           // 16-column blocks of a wave (ACT: three of a, three of b, then three of dh)
+    static constexpr int SA = 2, SB = ACT ? 4 : 3;   // k-steps in LDS
+    static constexpr int A_BYTES = BM * BK * 2, B_BYTES = ACT ? 2 * BN * BK * 2 : BN * BK * 2;
+    static constexpr int LDS = SA * A_BYTES + SB * B_BYTES;
+    static_assert(LDS <= 160 * 1024, "LDS of a CU");
+};
+
+// Sizes of a group in descending order: the expert of each rank in lane `rank`.  (The gradients of weights take as long as an expert has
+// rows: long ones go first.)
+__device__ __forceinline__ int by_size(int count, int E) {
+    const int lane = threadIdx.x & (kWave - 1);
+    int rank = 0;
+    for (int e = 0; e < E; ++e) {
+        const int c = MOE_READLANE(count, e);
+        rank += c > count || (c == count && e < lane) ? 1 : 0;
+    }
+    // lane r: the lane whose rank is r
+    return __builtin_amdgcn_ds_permute((lane < E ? rank : lane) << 2, lane);
+}
+
+// PARTS (DX): the k-steps of a tile are cut into g.k_parts runs, each stored in fp32 to an output of its own
+template <int OP, bool PARTS>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void grad_kernel(const GradArgs g) {
+    typedef Form<OP> F;
+    constexpr bool ACT = F::ACT, WGT = F::WGT;
+    constexpr int WAVES_M = F::WAVES_M, WAVES_N = F::WAVES_N, MB = F::MB, BN = F::BN, NI = F::NI, SA = F::SA, SB = F::SB;
+    constexpr int A_BYTES = F::A_BYTES, B_BYTES = F::B_BYTES, B_AT = SA * A_BYTES;
+    extern __shared__ __align__(16) char smem[];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int grp = wave >> 2, fw = wave & 3;
+    const int wm = wave / WAVES_N, wn = wave % WAVES_N;
+
+    // ---- the tile
+    int lo, hi, e, m0, m_end, n0, part = 0, which = 0;
+    int M_pitch, N, K;  // A's row pitch (transposed: its columns), output columns, k-values (of a pass)
+    group_bounds(g.offsets, g.E, g.P, lo, hi);
+    lo = min(max(lo, 0), g.P), hi = min(max(hi, lo), g.P);
+    const char *A0, *A1, *B0, *B1, *B2 = nullptr;
+    const size_t at_w = (size_t)g.d * g.F * 2;
+    if constexpr (WGT) {
+        // Strips of 256 hidden columns of an expert's three matrices, by all tiles across d; strips are dealt to the XCDs in turn.
+        const int dt = (g.d + 255) / 256, ft = (g.F + 255) / 256, slot = blockIdx.x >> 3;
+        const int strip = uniform_div(slot, dt) * 8 + (blockIdx.x & 7), across = slot - uniform_div(slot, dt) * dt;
+        const int rank = uniform_div(strip, 3 * ft), in = strip - rank * 3 * ft;
+        if (rank >= g.E) return;
+        e = MOE_READLANE(by_size(hi - lo, g.E), rank);
+        which = uniform_div(in, ft);
+        const int hidden = in - which * ft;
+        if (!(which == 0 ? g.gw_gate : which == 1 ? g.gw_up : g.gw_down)) return;
+        M_pitch = which == 2 ? g.d : g.F, N = which == 2 ? g.F : g.d;
+        m0 = (which == 2 ? across : hidden) * BM, n0 = (which == 2 ? hidden : across) * BN, m_end = M_pitch;
+        const int first = MOE_READLANE(lo, e);
+        K = MOE_READLANE(hi, e) - first;
+        A0 = A1 = static_cast<const char*>(which == 0 ? g.da : which == 1 ? g.db : g.gy) + (size_t)first * M_pitch * 2;
+        B0 = B1 = static_cast<const char*>(which == 2 ? g.h : g.x) + (size_t)first * N * 2;
+    } else {
+        N = ACT ? g.F : g.d, K = M_pitch = ACT ? g.d : g.F;
+        int nt;
+        const int n_tiles = (N + BN - 1) / BN, copies = PARTS ? g.k_parts : 1;
+        if (!find_tile<ACT ? 4 : kHiddenOperandBlock, 0>(lo, hi, g.E, BM, [&](int) INLINE { return n_tiles * copies; }, e, m0, m_end, nt)) return;
+        if (PARTS) {
+            part = uniform_div(nt, n_tiles);
+            nt -= part * n_tiles;
+        }
+        n0 = nt * BN;
+        A0 = static_cast<const char*>(ACT ? g.x : g.da), A1 = static_cast<const char*>(ACT ? g.gy : g.db);
+        B0 = static_cast<const char*>(g.w_gate) + e * at_w, B1 = static_cast<const char*>(g.w_up) + e * at_w;
+        if (ACT) B2 = static_cast<const char*>(g.w_down) + e * at_w;
+    }
+    const int nk = (K + BK - 1) / BK;              // k-steps of a pass
+    int v0 = 0, v_end = WGT ? nk : 2 * nk;         // those of this workgroup (ACT, DX: steps of the second pass from nk on)
+    if (PARTS) v0 = uniform_div(2 * nk * part, g.k_parts), v_end = uniform_div(2 * nk * (part + 1), g.k_parts);
+    const int rows_here = m_end - m0;
+    const unsigned pitch_a = (unsigned)M_pitch * 2, pitch_b = (unsigned)N * 2;  // bytes (pitch_b: operands read transposed)
+
+    // ---- fills.  Instruction p of wave w % 4 = fw writes the KB 4 p + fw of its operand's step; lane l the l-th 16 bytes of it.
+    const unsigned lds0 = (unsigned)(uintptr_t)(lds_char*)smem;
+    constexpr int PA = BM / 32;
+    constexpr int PB0 = ACT ? 6 : 8, PB1 = ACT ? 4 : 8;  // of B in the first and in the second pass
+    // rows of 128 bytes: row 8 (4 p + fw) + l / 8, slot l % 8 = chunk ^ (row / 2) % 8
+    const int k_row = fw * 8 + (lane >> 3);
+    const unsigned k_chunk = ((lane & 7) ^ (((fw & 1) << 2) | (lane >> 4))) * 16;
+    // rows of 512 bytes: row 2 (4 p + fw) + l / 32, slot l % 32 = chunk ^ 2 f, f = bits 0, 1 and 3 of the row
+    const int t_row = fw * 2 + (lane >> 5);
+    const int t_chunk = (lane & 31) ^ ((t_row & 3) << 1);  // (p odd: ^ 8)
+    unsigned off[8];
+    unsigned col[2] = {};
+    if (grp == 1 && !WGT) {
+#pragma unroll
+        for (int p = 0; p < PA; ++p) off[p] = (unsigned)min(m0 + k_row + 32 * p, m_end - 1) * pitch_a;
+    } else if (grp == 1) {
+#pragma unroll
+        for (int p = 0; p < 2; ++p) col[p] = (unsigned)min(m0 + (t_chunk ^ (p << 3)) * 8, M_pitch - 8) * 2;
+    } else if (ACT) {
+#pragma unroll
+        for (int p = 0; p < 3; ++p) off[p] = (unsigned)min(n0 + k_row + 32 * p, N - 1) * ((unsigned)K * 2);
+        // rows of 256 bytes, 12 of their 16 chunks in use: row 4 (4 p + fw) + l / 16
+        const int f = (lane >> 4) | (fw >> 1) << 2;
+        col[0] = (unsigned)min(n0 + min((lane & 15) ^ (f << 1), 11) * 8, N - 8) * 2;
+    } else {
+#pragma unroll
+        for (int p = 0; p < 2; ++p) col[p] = (unsigned)min(n0 + (t_chunk ^ (p << 3)) * 8, N - 8) * 2;
+    }
+    // instruction p of step v (of pass S: ACT's differ)
+    auto fill = [&](auto gc, auto sc, int v, int p) INLINE {
+        constexpr int GRP = decltype(gc)::value, S = decltype(sc)::value;
+        const bool second = !WGT && (ACT ? S == 1 : v >= nk);
+        const int t = second ? v - nk : v, left = K - t * BK;  // k-values from this step on
+        if constexpr (GRP == 1 && !WGT) {
+            const unsigned chunk = min(k_chunk, (unsigned)left * 2 - 16);
+            dma16<false>(lds0 + v % SA * A_BYTES + p * 4096 + fw * 1024, (second ? A1 : A0) + t * (BK * 2), off[p] + chunk);
+        } else if constexpr (GRP == 0 && ACT && S == 0) {
+            const unsigned chunk = min(k_chunk, (unsigned)left * 2 - 16);
+            dma16<false>(lds0 + B_AT + v % SB * B_BYTES + p * 4096 + fw * 1024, (p < 3 ? B0 : B1) + t * (BK * 2), off[p % 3] + chunk);
+        } else if constexpr (GRP == 0 && ACT) {
+            const int row = min(16 * p + 4 * fw + (lane >> 4), left - 1);
+            dma16<false>(lds0 + B_AT + v % SB * B_BYTES + p * 4096 + fw * 1024, B2 + (size_t)(t * BK) * pitch_b, (unsigned)row * pitch_b + col[0]);
+        } else {
+            const unsigned pitch = GRP == 1 ? pitch_a : pitch_b;
+            const char* const src = (GRP == 1 ? A0 : second ? B1 : B0) + (size_t)(t * BK) * pitch;
+            const unsigned slot = GRP == 1 ? v % SA * A_BYTES : B_AT + v % SB * B_BYTES;
+            const int row = min(8 * p + t_row, left - 1);
+            dma16<false>(lds0 + slot + p * 4096 + fw * 1024, src, (unsigned)row * pitch + col[p & 1]);
+        }
+    };
+
+    f32x4 acc[2 * MB][NI], acc2[ACT ? 2 * MB : 1][ACT ? 3 : 1];
+#pragma unroll
+    for (int mi = 0; mi < 2 * MB; ++mi)
+#pragma unroll
+        for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (ACT) {
+#pragma unroll
+        for (int mi = 0; mi < 2 * MB; ++mi)
+#pragma unroll
+            for (int ni = 0; ni < 3; ++ni) acc2[mi][ni] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const int live = min(MB, max(0, ((min(rows_here, BM) + 31) / 32 + WAVES_M - 1 - wm) / WAVES_M));
+
+    // ---- fragment reads.  Rows of 128 bytes: row l % 16 of a block, chunk 4 ks + l / 16.
+    const unsigned c16 = ((lane >> 4) ^ ((lane & 15) >> 1)) << 4;
+    const unsigned ra = lds0 + wm * 4096 + (lane & 15) * 128 + c16;
+    const unsigned rb = lds0 + B_AT + wn * 48 * 128 + (lane & 15) * 128 + c16;  // (ACT, first pass)
+    // rows read transposed: row 8 (l / 16) + (l % 16) / 4 (+ 4) of a 32-row half step, 8 bytes (l % 4) of unit u ^ f
+    const unsigned t_lane_row = 8 * (lane >> 4) + ((lane & 15) >> 2);
+    const unsigned t_swz = (((lane & 15) >> 2) | ((lane >> 4) & 1) << 2) << 5, t_byte = (lane & 3) * 8;
+
+    auto k_loop = [&](auto ma, auto gc) INLINE {
+        constexpr int MA = decltype(ma)::value, GRP = decltype(gc)::value, MR = MA > 0 ? MA : 1;
+        constexpr int NFA = WGT || MA == MB ? PA : std::min(PA, WAVES_M * (MA + 1) - 1);
+        constexpr int AHEAD = GRP == 0 ? SB - 1 : SA;
+        bf16x8 fa[2][2 * MR], fb[2][NI];
+        auto read = [&](auto sc, int v) INLINE {
+            constexpr int S = decltype(sc)::value, N_I = ACT && S == 1 ? 3 : NI;
+            const unsigned pa = v % SA * A_BYTES, pb = v % SB * B_BYTES;
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+                for (int ni = 0; ni < N_I; ++ni) {
+                    if constexpr (ACT && S == 0) {
+                        fb[ks][ni] = *reinterpret_cast<const __attribute__((address_space(3))) bf16x8*>(
+                            (uintptr_t)((rb ^ (ks << 6)) + pb + (ni / 3) * (96 * 128) + (ni % 3) * 2048));
+                    } else if constexpr (ACT) {
+                        const unsigned unit = (unsigned)(wn * 3 + ni) << 5;
+                        fb[ks][ni] = read_transposed(lds0 + B_AT + pb + t_lane_row * 256 + (unit ^ t_swz) + t_byte + ks * (32 * 256), 4 * 256);
+                    } else {
+                        const unsigned unit = (unsigned)(wn * NI + ni) << 5;
+                        fb[ks][ni] = read_transposed(lds0 + B_AT + pb + t_lane_row * 512 + (unit ^ t_swz) + t_byte + ks * (32 * 512), 4 * 512);
+                    }
+                }
+#pragma unroll
+                for (int mi = 0; mi < 2 * MA; ++mi) {
+                    if constexpr (WGT) {
+                        const unsigned unit = (unsigned)((wm + (mi >> 1) * WAVES_M) * 2 + (mi & 1)) << 5;
+                        fa[ks][mi] = read_transposed(lds0 + pa + t_lane_row * 512 + (unit ^ t_swz) + t_byte + ks * (32 * 512), 4 * 512);
+                    } else {
+                        fa[ks][mi] = *reinterpret_cast<const __attribute__((address_space(3))) bf16x8*>(
+                            (uintptr_t)((ra ^ (ks << 6)) + pa + (mi >> 1) * (WAVES_M * 4096) + (mi & 1) * 2048));
+                    }
+                }
+            }
+        };
+        // the last step of a pass: k-values past the end (copies of the last ones) are taken out of A
+        auto clear_past = [&](int left) INLINE {
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                if constexpr (WGT) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const bool past = ks * 32 + (lane >> 4) * 8 + j >= left;
+#pragma unroll
+                        for (int mi = 0; mi < 2 * MA; ++mi) fa[ks][mi][j] = past ? (bf16_t)0.f : fa[ks][mi][j];
+                    }
+                } else if (ks * 32 + (lane >> 4) * 8 >= left) {  // (a multiple of 8)
+#pragma unroll
+                    for (int mi = 0; mi < 2 * MA; ++mi) fa[ks][mi] = bf16x8{};
+                }
+            }
+        };
+        // products of a step of pass S, between them the fills of step vf of pass SF (< 0: none)
+        auto multiply = [&](auto sc, auto sf, int vf) INLINE {
+            constexpr int S = decltype(sc)::value, SF = decltype(sf)::value, N_I = ACT && S == 1 ? 3 : NI;
+            constexpr int NF = SF < 0 ? 0 : GRP == 1 ? NFA : SF == 0 ? PB0 : PB1;
+            constexpr int NM = MA * 4 * N_I, GAP = std::max(1, NM / std::max(1, NF));
+            int p = 0;
+#pragma unroll
+            for (int i = 0; i < NM; ++i) {
+                const int ni = i % N_I, mi = i / N_I % (2 * MR), ks = i / (N_I * 2 * MR);
+                f32x4& c = ACT && S == 1 ? acc2[ACT ? mi : 0][ACT ? ni : 0] : acc[mi][ni];
+                c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[ks][ni], fa[ks][mi], c, 0, 0, 0);
+                if (i % GAP == GAP - 1 && p < NF) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    fill(gc, sf, vf, p);
+                    ++p;
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+#pragma unroll
+            for (; p < NF; ++p) fill(gc, sf, vf, p);
+        };
+        // steps [from, to) of pass S while those AHEAD of them, of pass SF, are fetched
+        auto steps = [&](int from, int to, auto sc, auto sf) INLINE {
+            constexpr int S = decltype(sc)::value, SF = decltype(sf)::value;
+            constexpr int FLY = SF < 0 ? 0 : GRP == 0 ? (AHEAD - 1) * (SF == 0 ? PB0 : PB1) : (SA - 2) * NFA;
+            for (int v = from; v < to; ++v) {
+                if (MA > 0) {
+                    read(sc, v);
+                    // (DX: the first pass may end among steps that still fetch)
+                    if (SF != 0 || OP == GRAD_DX) {
+                        const int t = WGT || S == 0 ? (OP == GRAD_DX && v >= nk ? v - nk : v) : v - nk;
+                        if (t == nk - 1 && K % BK) clear_past(K - t * BK);
+                    }
+                }
+                if (GRP == 1) wait_vm<FLY>();  // A of step v + 1
+                phase_end();
+                multiply(sc, sf, v + AHEAD);
+                if (GRP == 0) wait_vm<FLY>();  // B of step v + 1
+                phase_end();
+            }
+        };
+        typedef std::integral_constant<int, 0> s0;
+        typedef std::integral_constant<int, 1> s1;
+        typedef std::integral_constant<int, -1> none;
+        const int nv = v_end - v0;
+        constexpr int NF0 = GRP == 1 ? NFA : PB0;
+#pragma unroll
+        for (int q = 0; q < AHEAD; ++q)
+            if (q < nv) {
+#pragma unroll
+                for (int p = 0; p < NF0; ++p) fill(gc, s0{}, v0 + q, p);
+            }
+        if (nv >= AHEAD) wait_vm<(AHEAD - 1) * NF0>();  // the first step has landed
+        else wait_vm<0>();
+        phase_end();
+        if (GRP == 1) phase_end();
+        if constexpr (ACT) {  // (nk >= AHEAD: run_grad_mfma)
+            steps(0, nk - AHEAD, s0{}, s0{});
+            steps(nk - AHEAD, nk, s0{}, s1{});
+            steps(nk, 2 * nk - AHEAD, s1{}, s1{});
+            steps(2 * nk - AHEAD, 2 * nk, s1{}, none{});
+        } else {
+            const int mid = max(v0, v_end - AHEAD);
+            steps(v0, mid, s0{}, s0{});
+            steps(mid, v_end, s0{}, none{});
+        }
+    };
+    auto loops = [&](auto ma) INLINE {
+        if (grp == 0) k_loop(ma, std::integral_constant<int, 0>{});
+        else k_loop(ma, std::integral_constant<int, 1>{});
+    };
+    if (v_end > v0) {  // (an expert without rows: zeros)
+        if (live == MB) loops(std::integral_constant<int, MB>{});
+        else if (live == 0) loops(std::integral_constant<int, 0>{});
+        else if (live == 1) loops(std::integral_constant<int, 1>{});
+        else if (live == 2) loops(std::integral_constant<int, (MB > 2 ? 2 : 1)>{});
+        else loops(std::integral_constant<int, (MB > 3 ? 3 : 1)>{});
+        if (grp == 0) phase_end();
+    }
+
+    // ---- epilogue: accumulator element i of a block is output column 4 (lane / 16) + i of row lane % 16.
+    if constexpr (PARTS) {
+        float* const out = g.parts + (size_t)part * g.P * N + (size_t)m0 * N + n0;
+#pragma unroll
+        for (int mi = 0; mi < 2 * MB; ++mi) {
+            if (mi / 2 >= live) continue;
+            const int row = (WAVES_M * (mi / 2) + wm) * 32 + mi % 2 * 16 + (lane & 15);
+#pragma unroll
+            for (int ni = 0; ni < NI; ++ni) {
+                const int c = (wn * NI + ni) * 16 + (lane >> 4) * 4;
+                if (row < rows_here && n0 + c < N) *reinterpret_cast<f32x4*>(out + (size_t)row * N + c) = acc[mi][ni];
+            }
+        }
+        return;
+    }
+    // Staged through LDS, 32 rows at a time in a region per wave, so that the tile leaves in 16-byte stores.
+    constexpr int OC = BN / WAVES_N, PITCH = OC * 2 + 16;
+    constexpr int LPR = OC / 8, RPI = 64 / LPR;
+    char* const region = smem + wave * (32 * PITCH);
+    char* const wr = region + (lane & 15) * PITCH + (lane >> 4) * 8;
+    const int rd_row = lane / LPR, rd_chunk = lane % LPR;
+    const int c0 = wn * OC + rd_chunk * 8;
+    auto leave = [&](int rbk, bf16_t* out) INLINE {  // the staged 32 rows
+#pragma unroll
+        for (int it = 0; it < (32 + RPI - 1) / RPI; ++it) {
+            const int r = it * RPI + rd_row;
+            if ((64 % LPR || 32 % RPI) && (rd_row >= RPI || r >= 32)) continue;
+            const uint4 v = *reinterpret_cast<const uint4*>(region + r * PITCH + rd_chunk * 16);
+            if (rbk + r < rows_here && n0 + c0 < N) *reinterpret_cast<uint4*>(out + (size_t)(rbk + r) * N + c0) = v;
+        }
+    };
+    const size_t at0 = (size_t)m0 * N + n0;
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+        if (mb >= live) continue;
+        const int rbk = (WAVES_M * mb + wm) * 32;
+        if constexpr (ACT) {
+            static_for<3>([&](auto what) INLINE {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int nb = 0; nb < 3; ++nb) {
+                        bf16x4 o;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const ActGrad v = act_grad(acc[2 * mb + h][nb][j], acc[2 * mb + h][nb + 3][j], acc2[2 * mb + h][nb][j]);
+                            o[j] = (bf16_t)(what == 0 ? v.h : what == 1 ? v.da : v.db);
+                        }
+                        *reinterpret_cast<bf16x4*>(wr + h * 16 * PITCH + nb * 32) = o;
+                    }
+                leave(rbk, static_cast<bf16_t*>(what == 0 ? g.h : what == 1 ? g.da : g.db) + at0);
+            });
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int nb = 0; nb < NI; ++nb) {
+                    bf16x4 o;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[j] = (bf16_t)acc[2 * mb + h][nb][j];
+                    *reinterpret_cast<bf16x4*>(wr + h * 16 * PITCH + nb * 32) = o;
+                }
+            bf16_t* const out = static_cast<bf16_t*>(!WGT ? g.gx : which == 0 ? g.gw_gate : which == 1 ? g.gw_up : g.gw_down);
+            leave(rbk, out + (WGT ? (size_t)e * g.d * g.F : 0) + at0);
+        }
+    }
+}
+
+template <int OP, bool PARTS>
+int launch(const GradArgs& g, int grid, hipStream_t st) {
+    static std::atomic<uint64_t> lds_allowed;
+    const auto kern = grad_kernel<OP, PARTS>;
+    if (allow_dynamic_lds(reinterpret_cast<const void*>(kern), Form<OP>::LDS, lds_allowed) != MOE_OK) return MOE_ERR_LAUNCH;
+    hipLaunchKernelGGL(kern, dim3(grid), dim3(kThreads), Form<OP>::LDS, st, g);
+    return launch_status();
+}
+
+}  // namespace
+
+// Offsets within an operand's rows are 32 bits, and a pass has as many k-steps as are fetched ahead of the first
+bool grad_mfma_supported(const GradArgs& g) {
+    const long long d = g.d, F = g.F, P = g.P;
+    return d > 2 * BK && F > 2 * BK && P * d * 2 < (1ll << 32) && P * F * 2 < (1ll << 32) && d * F * 2 < (1ll << 32);
+}
+
+int run_grad_mfma(const GradArgs& g, GradOp op, hipStream_t st) {
+    if (op == GRAD_WEIGHTS) {
+        const int strips = g.E * 3 * ((g.F + 255) / 256);
+        return launch<GRAD_WEIGHTS, false>(g, (strips + 7) / 8 * 8 * ((g.d + 255) / 256), st);
+    }
+    const int m = m_tiles_bound(g.P, g.E, BM);
+    if (op == GRAD_ACT) return launch<GRAD_ACT, false>(g, find_tile_grid(m * ((g.F + Form<GRAD_ACT>::BN - 1) / Form<GRAD_ACT>::BN), 0), st);
+    return launch<GRAD_DX, false>(g, find_tile_grid(m * ((g.d + 255) / 256), 0), st);
+}
+
+}  // namespace moe
