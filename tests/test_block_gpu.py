@@ -1,0 +1,299 @@
+"""The block around a layer (norms, gates, dropout, scaled residual) and its gradient, on the GPU, against plain implementations in 64 bits
+with bounds from the roundings on the way; the stack of such blocks; a training step of one, end to end and in a graph."""
+import importlib.util
+import os
+
+import pytest
+import torch
+
+import paper_2503_00245_amd as pkg
+from tests import training_oracle as to
+from tests.test_training_gpu import CODE, DTYPES, dev, gen, rnd
+
+pytestmark = pytest.mark.gpu
+
+
+def on(t):
+    return None if t is None else t.to(dev())
+
+
+def config(g, T, d, what, dropout=0.0):
+    """what: letters of p(ost norm), g(ate), t(oken gate)"""
+    cfg = {"eps": 1e-5, "skip_scale": 0.75, "block_scale": 1.25, "dropout": dropout}
+    cfg["post_w"] = 1 + rnd(g, d, std=0.2) if "p" in what else None
+    cfg["gate"] = rnd(g, d) if "g" in what else None
+    cfg["token_gate"] = rnd(g, T) if "t" in what else None
+    cfg["rng"] = torch.tensor([0x1234567890ABCDEF, -3]) if dropout else None
+    return cfg
+
+
+def block_of(cfg):
+    return pkg.make_block(**{n: on(v) if torch.is_tensor(v) else v for n, v in cfg.items()})
+
+
+SHAPES = [(1, 8), (1, 2048), (3, 40), (17, 512), (5, 520), (130, 432), (2049, 1440), (2500, 64), (3, 8192), (2, 8200), (1, 32768), (600, 2056)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("what", ["", "p", "pg", "pgt", "t"])
+@pytest.mark.parametrize("T,d", SHAPES)
+def test_block(T, d, what, dtype):
+    dt, g = DTYPES[dtype], gen(T * 7 + d)
+    cfg = config(g, T, d, what)
+    x, b, w = rnd(g, T, d, dtype=dt), rnd(g, T, d, std=0.3, dtype=dt), 1 + rnd(g, d, std=0.2)
+    b[T // 2] = 0  # a row of zeros: its norm is zero
+    blk = block_of(cfg)
+    y, n = (torch.full((T, d), float("nan"), dtype=dt, device=dev()) for _ in range(2))
+    pkg.moe_block_norm(blk, on(x), on(b), on(w), y, n)
+    to.near(y, to.block(cfg, x, b, None, dt), "y")
+    to.near(n, to.opened(y.cpu(), w, cfg["eps"], dt), "n")
+    # the end alone, in place; the start alone
+    place = on(x).clone()
+    pkg.moe_block_norm(blk, place, on(b), None, place, None)
+    assert torch.equal(place, y)
+    alone = torch.full_like(n, float("nan"))
+    pkg.moe_block_norm(blk, y, None, on(w), None, alone)
+    assert torch.equal(alone, n)
+
+    gy, gn = rnd(g, T, d, dtype=dt), rnd(g, T, d, dtype=dt)
+    ws = pkg.alloc_block_workspace(T, d, dev())
+    for with_y, with_n in ((True, True), (True, False), (False, True)):
+        u, v = gy if with_y else None, gn if with_n else None
+        want = to.block_grad(cfg, u, v, y.cpu() if with_n else None, b, w if with_n else None, None, dt)
+        out = {m: torch.full((T, d), float("nan"), dtype=dt, device=dev()) for m in ("x", "b")}
+        names = [m for m, size in (("open_w", d), ("post_w", d), ("gate", d), ("token_gate", T)) if m in want]
+        for m in names:
+            out[m] = torch.full((T if m == "token_gate" else d,), float("nan"), device=dev())
+
+        def call(o, workspace=ws, ow=on(w) if with_n else None):
+            pkg.moe_block_norm_backward(blk, on(u), on(v), y if with_n else None, on(b), ow, o["x"], o["b"], o.get("open_w"), o.get("post_w"),
+                                        o.get("gate"), o.get("token_gate"), workspace)
+        call(out)
+        for m in out:
+            to.near(out[m], want[m], m)
+        few = {m: torch.full_like(out[m], float("nan")) for m in ("x", "b")}  # the rows' gradients alone, without a workspace
+        call(few, None)
+        assert torch.equal(few["x"], out["x"]) and torch.equal(few["b"], out["b"])
+        if with_y:
+            inplace = dict(out, x=on(u).clone())
+            pkg.moe_block_norm_backward(blk, inplace["x"], on(v), y if with_n else None, on(b), on(w) if with_n else None, inplace["x"], few["b"], None, None,
+                                        None, None, None)
+            assert torch.equal(inplace["x"], out["x"])
+    # the start of a block alone
+    for u in (gy, None):
+        want = to.block_grad(cfg, u, gn, y.cpu(), None, w, None, dt)
+        gx, gw = torch.full_like(y, float("nan")), torch.full((d,), float("nan"), device=dev())
+        pkg.moe_block_norm_backward(blk, on(u), on(gn), y, None, on(w), gx, None, gw, workspace=ws)
+        to.near(gx, want["x"], "x alone")
+        to.near(gw, want["open_w"], "open_w alone")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,d,p", [(1, 8, 0.5), (33, 72, 0.1), (2100, 24, 0.25), (5, 2048, 0.999), (3, 520, 1e-7), (4, 64, 0.99999)])
+def test_dropout(T, d, p, dtype):
+    dt, g = DTYPES[dtype], gen(T + d)
+    cfg = config(g, T, d, "pgt", p)
+    mask = to.kept(T, d, p, cfg["rng"].tolist())
+    x, b = rnd(g, T, d, dtype=dt), rnd(g, T, d, dtype=dt)
+    blk = block_of(cfg)
+    y = torch.empty(T, d, dtype=dt, device=dev())
+    pkg.moe_block_norm(blk, on(x), on(b), None, y, None)
+    to.near(y, to.block(cfg, x, b, mask, dt), "y")
+    gy = rnd(g, T, d, dtype=dt)
+    want = to.block_grad(cfg, gy, None, None, b, None, mask, dt)
+    out = {m: torch.empty(want[m][0].shape, dtype=dt if m in "xb" else torch.float32, device=dev()) for m in want}
+    pkg.moe_block_norm_backward(blk, on(gy), None, None, on(b), None, out["x"], out["b"], None, out["post_w"], out["gate"], out["token_gate"],
+                                pkg.alloc_block_workspace(T, d, dev()))
+    for m in want:
+        to.near(out[m], want[m], m)
+
+
+def test_dropout_takes_infinities_out():
+    # without a norm, what is dropped has no part in the result or in any gradient, whatever it is
+    T, d = 4, 64
+    cfg = config(gen(3), T, d, "g", 0.5)
+    mask = to.kept(T, d, 0.5, cfg["rng"].tolist())
+    x, gy = rnd(gen(4), T, d), rnd(gen(5), T, d)
+    b = torch.where(mask, rnd(gen(6), T, d), float("inf"))
+    blk = block_of(cfg)
+    y, gx, gb, gg = (torch.empty(T, d, device=dev()) for _ in range(4))
+    gg, tg = torch.empty(d, device=dev()), torch.empty(T, device=dev())
+    pkg.moe_block_norm(blk, on(x), on(b), None, y, None)
+    fine = torch.where(mask, b, 0.0)
+    to.near(y, to.block(cfg, x, fine, mask, torch.float32))
+    pkg.moe_block_norm_backward(blk, on(gy), None, None, on(b), None, gx, gb, None, None, gg, tg, pkg.alloc_block_workspace(T, d, dev()))
+    want = to.block_grad(cfg, gy, None, None, fine, None, mask, torch.float32)
+    for m, o in (("x", gx), ("gate", gg), ("token_gate", tg), ("b", gb)):
+        to.near(o, want[m], m)
+
+
+def test_no_tokens_give_sums_of_zero():
+    d = 72
+    blk = block_of(config(gen(1), 0, d, "pg"))
+    none = torch.empty(0, d, device=dev())
+    w = torch.ones(d, device=dev())
+    pkg.moe_block_norm(blk, none, none, w, none.clone(), none.clone())
+    sums = [torch.full((d,), float("nan"), device=dev()) for _ in range(3)]
+    pkg.moe_block_norm_backward(blk, none, none, none, none, w, none.clone(), none.clone(), *sums, None, pkg.alloc_block_workspace(0, d, dev()))
+    assert all((s == 0).all() for s in sums)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [1, 2, 33])
+def test_stack_of_blocks_is_its_calls_one_by_one(T, dtype):
+    dt, d, F, E, k, L = DTYPES[dtype], 128, 256, 8, 2, 3
+    g = gen(T)
+    shape = pkg.make_shape(T, d, F, E, k, act_dtype=CODE[dt])
+    kept = [{n: rnd(g, *s, std=s[-1] ** -0.5, dtype=torch.float32 if n == "router_w" else dt).to(dev())
+             for n, s in (("router_w", (E, d)), ("w_gate", (E, F, d)), ("w_up", (E, F, d)), ("w_down", (E, d, F)))} for _ in range(L)]
+    layers = [pkg.make_weights(w) for w in kept]
+    cfgs = [config(g, T, d, w) for w in ("pg", "pgt", "")]
+    blocks = [block_of(c) for c in cfgs]
+    open_w = [on(1 + rnd(g, d, std=0.2)) for _ in range(L)]
+    x = on(rnd(g, T, d, dtype=dt))
+    y, trace = torch.empty_like(x), torch.empty(L, T, k, dtype=torch.int32, device=dev())
+    ws = pkg.alloc_block_stack_workspace(shape, dev())
+    before = x.clone()
+    pkg.moe_block_stack_forward(shape, layers, blocks, open_w, x, y, trace, ws)
+    assert torch.equal(x, before)
+    n, b, cur, idx = torch.empty_like(x), torch.empty_like(x), x.clone(), torch.empty(T, k, dtype=torch.int32, device=dev())
+    lws = pkg.alloc_workspace(shape, dev())
+    for l in range(L):
+        pkg.moe_block_norm(blocks[max(l - 1, 0)], cur, None, open_w[l], None, n)
+        to.near(n, to.opened(cur.cpu(), open_w[l].cpu(), 1e-5, dt), "n")
+        pkg.moe_forward(shape, layers[l], n, b, idx, None, lws)
+        assert torch.equal(idx, trace[l])
+        nxt = torch.empty_like(x)
+        pkg.moe_block_norm(blocks[l], cur, b, None, nxt, None)
+        to.near(nxt, to.block(cfgs[l], cur.cpu(), b.cpu(), None, dt), "y")
+        cur = nxt
+    assert torch.equal(cur, y)
+
+
+def test_numbers_of_a_captured_step_come_from_the_device():
+    # a graph replayed with other numbers in rng gives other masks, each the eager call's
+    T, d = 64, 256
+    g = gen(11)
+    cfg = config(g, T, d, "pg", 0.3)
+    rng = on(cfg["rng"])
+    blk = pkg.make_block(**{**{n: on(v) if torch.is_tensor(v) else v for n, v in cfg.items()}, "rng": rng})
+    x, b, w, gy, gn = (on(rnd(g, T, d)) for _ in range(5))
+    w = w[0].contiguous()
+    y, n, gx, gb = (torch.empty_like(x) for _ in range(4))
+    sums = [torch.empty(d, device=dev()) for _ in range(3)]
+    ws = pkg.alloc_block_workspace(T, d, dev())
+
+    def step():
+        pkg.moe_block_norm(blk, x, b, w, y, n)
+        pkg.moe_block_norm_backward(blk, gy, gn, y, b, w, gx, gb, *sums, None, ws)
+
+    def results():
+        torch.cuda.synchronize()
+        return [t.clone() for t in (y, n, gx, gb, *sums)]
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    seen = []
+    for i in range(4):
+        rng.copy_(torch.tensor([77 + i, i << 40]))
+        graph.replay()
+        replayed = results()
+        step()
+        assert all(torch.equal(p, q) for p, q in zip(replayed, results()))
+        seen.append(replayed[0])
+    assert not torch.equal(seen[0], seen[1])
+
+
+def _example():
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "training_step.py")
+    spec = importlib.util.spec_from_file_location("training_step", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    return m
+
+
+@pytest.mark.parametrize("dtype,dropout,masked", [("f32", 0.0, 0.0), ("f32", 0.25, 0.2), ("bf16", 0.1, 0.0)])
+def test_training_step_of_a_block(dtype, dropout, masked):
+    """The example's step, its gradients against automatic differentiation of the whole block in 64 bits.
+
+    fp32: a result passes through sums of at most d + F + E + T terms in a row (2 d + F forward, as many back), 2^-24 each at worst, on
+    quantities that the softmax, the norms and the products' conditions enlarge by less than 32: 2^-24 * 2 * (2 d + F) * 32 of the norm.  bf16: n, rows,
+    h, da, db, the experts' output, b, and every gradient on the way back are rounded, 16 in a row, 2^-8 each, added up at worst: 2^-4."""
+    ex, T, d, F, E, k = _example(), 40, 64, 136, 8, 2
+    layer = ex.Block(T, d, F, E, k, DTYPES[dtype], dropout, seed=3)
+    g = gen(2)
+    x, gy = rnd(g, T, d, dtype=DTYPES[dtype]), rnd(g, T, d, dtype=DTYPES[dtype])
+    pad = torch.rand(T, generator=g) < masked
+    y, grads, idx = layer.step(on(x), on(gy), on(pad))
+    p = {n: v.detach().cpu().double().requires_grad_(v.is_floating_point()) for n, v in layer.weights.items()}
+    p.update(idx=idx.cpu().long().clamp(min=0), eps=layer.eps, block_scale=layer.block_scale)
+    xx = x.double().requires_grad_(True)
+    mask = to.kept(T, d, dropout, layer.rng.tolist()).double() if dropout else None
+    live = ~pad
+    out = to.step({**p, "x": xx, "idx": p["idx"]}, mask, dropout)
+    out = torch.where(live[:, None], out, xx)  # padding: no expert, no branch
+    limit = 2 ** -24 * 2 * (2 * d + F) * 32 if dtype == "f32" else 2.0 ** -4
+    names = [n for n in grads if n != "x"]
+    want = torch.autograd.grad(out, [xx] + [p[n] for n in names], gy.double())
+    rel = lambda a, b: float((a.detach().cpu().double() - b).norm() / b.norm())  # noqa: E731
+    assert rel(y, out.detach()) < limit
+    for n, w in zip(["x"] + names, want):
+        assert rel(grads[n], w) < limit, n
+
+
+def test_training_steps_in_graphs_replay_what_the_eager_step_does():
+    ex = _example()
+    layer = ex.Block(48, 64, 136, 8, 2, torch.bfloat16, 0.1, seed=4)
+    g = gen(9)
+    x, gy, pad = on(rnd(g, 48, 64, dtype=torch.bfloat16)), on(rnd(g, 48, 64, dtype=torch.bfloat16)), on(torch.zeros(48, dtype=torch.bool))
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        layer.step(x, gy, pad)
+    torch.cuda.synchronize()
+    graphs, outs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()], []
+    for graph in graphs:  # two graphs that share the layer's workspaces
+        with torch.cuda.graph(graph):
+            outs.append(layer.step(x, gy, pad))
+    for i in range(3):
+        x.copy_(rnd(g, 48, 64, dtype=torch.bfloat16))
+        for graph, (y, grads, _) in zip(graphs, outs):
+            graph.replay()
+            torch.cuda.synchronize()
+            y2, grads2, _ = layer.step(x, gy, pad)
+            torch.cuda.synchronize()
+            assert torch.equal(y, y2)
+            assert all(torch.equal(grads[n], grads2[n]) for n in grads)
+
+
+def test_calls_on_two_streams_do_not_meet():
+    g = gen(21)
+    T, d = 300, 520
+    cfg = config(g, T, d, "pg")
+    blk = block_of(cfg)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    sets = []
+    for _ in streams:
+        x, b, w, gy, gn = (on(rnd(g, T, d)) for _ in range(5))
+        sets.append((x, b, w[0].contiguous(), gy, gn, [torch.empty_like(x) for _ in range(4)], [torch.empty(d, device=dev()) for _ in range(3)],
+                     pkg.alloc_block_workspace(T, d, dev())))
+    torch.cuda.synchronize()
+
+    def call(s):
+        x, b, w, gy, gn, (y, n, gx, gb), sums, ws = s
+        pkg.moe_block_norm(blk, x, b, w, y, n)
+        pkg.moe_block_norm_backward(blk, gy, gn, y, b, w, gx, gb, *sums, None, ws)
+        return [y, n, gx, gb, *sums]
+    for _ in range(5):
+        for st, s in zip(streams, sets):
+            with torch.cuda.stream(st):
+                call(s)
+    torch.cuda.synchronize()
+    for s in sets:
+        got = [t.clone() for t in (*s[5], *s[6])]
+        alone = call(s)
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(got, alone))
