@@ -188,11 +188,12 @@ int run_plain(const GradArgs& g, GradOp op, hipStream_t st) {
 }
 
 struct GradLayout {
-    size_t da, db, h, total;
+    size_t da, db, h, parts, total;
 };
 GradLayout grad_layout(const moe_shape& s) {
     const size_t hidden = round_up((size_t)s.n_tokens * s.top_k * s.d_ff * elt_size(s.act_dtype), 256);
-    return GradLayout{0, hidden, 2 * hidden, 3 * hidden};
+    const size_t parts = s.act_dtype == MOE_BF16 ? round_up(grad_parts_bytes((long long)s.n_tokens * s.top_k, s.d_model), 256) : 0;
+    return GradLayout{0, hidden, 2 * hidden, 3 * hidden, 3 * hidden + parts};
 }
 
 int validate_grad(const moe_shape* s) {
@@ -250,7 +251,7 @@ extern "C" int moe_expert_ffn_backward(const moe_shape* shape, const moe_weights
     if (!any_w && !grad_x_perm) return MOE_OK;
     char* const ws = static_cast<char*>(workspace);
     g.x = x_perm, g.gy = grad_y_perm, g.w_gate = weights->w_gate, g.w_up = weights->w_up, g.w_down = weights->w_down;
-    g.da = ws + l.da, g.db = ws + l.db, g.h = ws + l.h, g.offsets = expert_offsets;
+    g.da = ws + l.da, g.db = ws + l.db, g.h = ws + l.h, g.parts = reinterpret_cast<float*>(ws + l.parts), g.offsets = expert_offsets;
     const bool mfma = s.act_dtype == MOE_BF16 && grad_mfma_supported(g);
     auto run = [&](GradOp op) { return mfma ? run_grad_mfma(g, op, st) : run_grad_plain(g, op, s.act_dtype, st); };
     rc = run(GRAD_ACT);

@@ -21,6 +21,7 @@
 #include "lds_fill.h"
 
 #include <algorithm>
+#include <cmath>
 
 namespace moe {
 
@@ -29,6 +30,7 @@ namespace {
 #define INLINE __attribute__((always_inline))
 
 constexpr int BM = 256, BK = 64, kThreads = 512;
+constexpr int kSplitSlots = 32;  // one workgroup per CU
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
@@ -110,7 +112,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         N = ACT ? g.F : g.d, K = M_pitch = ACT ? g.d : g.F;
         int nt;
         const int n_tiles = (N + BN - 1) / BN, copies = PARTS ? g.k_parts : 1;
-        if (!find_tile<ACT ? 4 : kHiddenOperandBlock, 0>(lo, hi, g.E, BM, [&](int) INLINE { return n_tiles * copies; }, e, m0, m_end, nt)) return;
+        if (!find_tile<ACT ? 4 : kHiddenOperandBlock, kSplitSlots>(lo, hi, g.E, BM, [&](int) INLINE { return n_tiles * copies; }, e, m0, m_end, nt)) return;
         if (PARTS) {
             part = uniform_div(nt, n_tiles);
             nt -= part * n_tiles;
@@ -136,44 +138,50 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     // rows of 512 bytes: row 2 (4 p + fw) + l / 32, slot l % 32 = chunk ^ 2 f, f = bits 0, 1 and 3 of the row
     const int t_row = fw * 2 + (lane >> 5);
     const int t_chunk = (lane & 31) ^ ((t_row & 3) << 1);  // (p odd: ^ 8)
-    unsigned off[8];
-    unsigned col[2] = {};
+    // Lane offsets are kept whole: beside them a fill takes scalar operations only.  The last step of ACT and DX is fetched as the last 64
+    // k-values; those that it shares with the step before are taken out of A's fragments.
+    unsigned off[8], col[2] = {};
     if (grp == 1 && !WGT) {
 #pragma unroll
-        for (int p = 0; p < PA; ++p) off[p] = (unsigned)min(m0 + k_row + 32 * p, m_end - 1) * pitch_a;
+        for (int p = 0; p < PA; ++p) off[p] = (unsigned)min(m0 + k_row + 32 * p, m_end - 1) * pitch_a + k_chunk;
     } else if (grp == 1) {
 #pragma unroll
         for (int p = 0; p < 2; ++p) col[p] = (unsigned)min(m0 + (t_chunk ^ (p << 3)) * 8, M_pitch - 8) * 2;
     } else if (ACT) {
 #pragma unroll
-        for (int p = 0; p < 3; ++p) off[p] = (unsigned)min(n0 + k_row + 32 * p, N - 1) * ((unsigned)K * 2);
+        for (int p = 0; p < 3; ++p) off[p] = (unsigned)min(n0 + k_row + 32 * p, N - 1) * ((unsigned)K * 2) + k_chunk;
         // rows of 256 bytes, 12 of their 16 chunks in use: row 4 (4 p + fw) + l / 16
         const int f = (lane >> 4) | (fw >> 1) << 2;
-        col[0] = (unsigned)min(n0 + min((lane & 15) ^ (f << 1), 11) * 8, N - 8) * 2;
+        col[0] = (unsigned)min(n0 + min((lane & 15) ^ (f << 1), 11) * 8, N - 8) * 2 + (unsigned)(4 * fw + (lane >> 4)) * pitch_b;
     } else {
 #pragma unroll
         for (int p = 0; p < 2; ++p) col[p] = (unsigned)min(n0 + (t_chunk ^ (p << 3)) * 8, N - 8) * 2;
     }
-    // instruction p of step v (of pass S: ACT's differ)
+    if (!(ACT || (grp == 1 && !WGT))) {
+#pragma unroll
+        for (int p = 0; p < 2; ++p) col[p] += (unsigned)t_row * (grp == 1 ? pitch_a : pitch_b);
+    }
+    // instruction p of step v (of pass S: ACT's differ; WGT: 2 is a last step of fewer than 64 rows, the others of which are the last again)
     auto fill = [&](auto gc, auto sc, int v, int p) INLINE {
         constexpr int GRP = decltype(gc)::value, S = decltype(sc)::value;
         const bool second = !WGT && (ACT ? S == 1 : v >= nk);
-        const int t = second ? v - nk : v, left = K - t * BK;  // k-values from this step on
+        const int t = second ? v - nk : v, k0 = WGT ? t * BK : min(t * BK, K - BK);
+        const unsigned slot = lds0 + (GRP == 1 ? v % SA * A_BYTES : B_AT + v % SB * B_BYTES) + fw * 1024 + p * 4096;
         if constexpr (GRP == 1 && !WGT) {
-            const unsigned chunk = min(k_chunk, (unsigned)left * 2 - 16);
-            dma16<false>(lds0 + v % SA * A_BYTES + p * 4096 + fw * 1024, (second ? A1 : A0) + t * (BK * 2), off[p] + chunk);
+            dma16<false>(slot, (second ? A1 : A0) + k0 * 2, off[p]);
         } else if constexpr (GRP == 0 && ACT && S == 0) {
-            const unsigned chunk = min(k_chunk, (unsigned)left * 2 - 16);
-            dma16<false>(lds0 + B_AT + v % SB * B_BYTES + p * 4096 + fw * 1024, (p < 3 ? B0 : B1) + t * (BK * 2), off[p % 3] + chunk);
+            dma16<false>(slot, (p < 3 ? B0 : B1) + k0 * 2, off[p % 3]);
         } else if constexpr (GRP == 0 && ACT) {
-            const int row = min(16 * p + 4 * fw + (lane >> 4), left - 1);
-            dma16<false>(lds0 + B_AT + v % SB * B_BYTES + p * 4096 + fw * 1024, B2 + (size_t)(t * BK) * pitch_b, (unsigned)row * pitch_b + col[0]);
+            dma16<false>(slot, B2 + (size_t)(unsigned)(k0 + 16 * p) * pitch_b, col[0]);
         } else {
             const unsigned pitch = GRP == 1 ? pitch_a : pitch_b;
-            const char* const src = (GRP == 1 ? A0 : second ? B1 : B0) + (size_t)(t * BK) * pitch;
-            const unsigned slot = GRP == 1 ? v % SA * A_BYTES : B_AT + v % SB * B_BYTES;
-            const int row = min(8 * p + t_row, left - 1);
-            dma16<false>(lds0 + slot + p * 4096 + fw * 1024, src, (unsigned)row * pitch + col[p & 1]);
+            const char* const src = GRP == 1 ? A0 : second ? B1 : B0;
+            if constexpr (S == 2) {
+                const int row = min(8 * p + t_row, K - 1 - k0);
+                dma16<false>(slot, src + (size_t)(unsigned)k0 * pitch, col[p & 1] + (unsigned)(row - t_row) * pitch);
+            } else {
+                dma16<false>(slot, src + (size_t)(unsigned)(k0 + 8 * p) * pitch, col[p & 1]);
+            }
         }
     };
 
@@ -195,8 +203,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     const unsigned ra = lds0 + wm * 4096 + (lane & 15) * 128 + c16;
     const unsigned rb = lds0 + B_AT + wn * 48 * 128 + (lane & 15) * 128 + c16;  // (ACT, first pass)
     // rows read transposed: row 8 (l / 16) + (l % 16) / 4 (+ 4) of a 32-row half step, 8 bytes (l % 4) of unit u ^ f
-    const unsigned t_lane_row = 8 * (lane >> 4) + ((lane & 15) >> 2);
-    const unsigned t_swz = (((lane & 15) >> 2) | ((lane >> 4) & 1) << 2) << 5, t_byte = (lane & 3) * 8;
+    constexpr int T_ROW = ACT ? 256 : 512;
+    const unsigned t_swz = (((lane & 15) >> 2) | ((lane >> 4) & 1) << 2) << 5;
+    const unsigned t_lane = lds0 + (8 * (lane >> 4) + ((lane & 15) >> 2)) * T_ROW + (lane & 3) * 8;
 
     auto k_loop = [&](auto ma, auto gc) INLINE {
         constexpr int MA = decltype(ma)::value, GRP = decltype(gc)::value, MR = MA > 0 ? MA : 1;
@@ -206,6 +215,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         auto read = [&](auto sc, int v) INLINE {
             constexpr int S = decltype(sc)::value, N_I = ACT && S == 1 ? 3 : NI;
             const unsigned pa = v % SA * A_BYTES, pb = v % SB * B_BYTES;
+            // (an address for each unit is made here, of two instructions; kept over the loop, they did not fit the registers)
+            unsigned swz = t_swz;
+#if defined(__HIP_DEVICE_COMPILE__)
+            if (!ACT || S == 1) asm volatile("" : "+v"(swz));
+#endif
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) {
 #pragma unroll
@@ -215,17 +229,17 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                             (uintptr_t)((rb ^ (ks << 6)) + pb + (ni / 3) * (96 * 128) + (ni % 3) * 2048));
                     } else if constexpr (ACT) {
                         const unsigned unit = (unsigned)(wn * 3 + ni) << 5;
-                        fb[ks][ni] = read_transposed(lds0 + B_AT + pb + t_lane_row * 256 + (unit ^ t_swz) + t_byte + ks * (32 * 256), 4 * 256);
+                        fb[ks][ni] = read_transposed((unit ^ swz) + (t_lane + B_AT + pb) + ks * (32 * T_ROW), 4 * T_ROW);
                     } else {
                         const unsigned unit = (unsigned)(wn * NI + ni) << 5;
-                        fb[ks][ni] = read_transposed(lds0 + B_AT + pb + t_lane_row * 512 + (unit ^ t_swz) + t_byte + ks * (32 * 512), 4 * 512);
+                        fb[ks][ni] = read_transposed((unit ^ swz) + (t_lane + B_AT + pb) + ks * (32 * T_ROW), 4 * T_ROW);
                     }
                 }
 #pragma unroll
                 for (int mi = 0; mi < 2 * MA; ++mi) {
                     if constexpr (WGT) {
                         const unsigned unit = (unsigned)((wm + (mi >> 1) * WAVES_M) * 2 + (mi & 1)) << 5;
-                        fa[ks][mi] = read_transposed(lds0 + pa + t_lane_row * 512 + (unit ^ t_swz) + t_byte + ks * (32 * 512), 4 * 512);
+                        fa[ks][mi] = read_transposed((unit ^ swz) + (t_lane + pa) + ks * (32 * T_ROW), 4 * T_ROW);
                     } else {
                         fa[ks][mi] = *reinterpret_cast<const __attribute__((address_space(3))) bf16x8*>(
                             (uintptr_t)((ra ^ (ks << 6)) + pa + (mi >> 1) * (WAVES_M * 4096) + (mi & 1) * 2048));
@@ -233,18 +247,18 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                 }
             }
         };
-        // the last step of a pass: k-values past the end (copies of the last ones) are taken out of A
-        auto clear_past = [&](int left) INLINE {
+        // the last step of a pass, `left` k-values of which are its own: the others are taken out of A
+        auto clear_others = [&](int left) INLINE {
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) {
-                if constexpr (WGT) {
+                if constexpr (WGT) {  // they are the last ones
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         const bool past = ks * 32 + (lane >> 4) * 8 + j >= left;
 #pragma unroll
                         for (int mi = 0; mi < 2 * MA; ++mi) fa[ks][mi][j] = past ? (bf16_t)0.f : fa[ks][mi][j];
                     }
-                } else if (ks * 32 + (lane >> 4) * 8 >= left) {  // (a multiple of 8)
+                } else if (ks * 32 + (lane >> 4) * 8 < BK - left) {  // they are the first ones (a multiple of 8)
 #pragma unroll
                     for (int mi = 0; mi < 2 * MA; ++mi) fa[ks][mi] = bf16x8{};
                 }
@@ -253,7 +267,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         // products of a step of pass S, between them the fills of step vf of pass SF (< 0: none)
         auto multiply = [&](auto sc, auto sf, int vf) INLINE {
             constexpr int S = decltype(sc)::value, SF = decltype(sf)::value, N_I = ACT && S == 1 ? 3 : NI;
-            constexpr int NF = SF < 0 ? 0 : GRP == 1 ? NFA : SF == 0 ? PB0 : PB1;
+            constexpr int NF = SF < 0 ? 0 : GRP == 1 ? NFA : SF == 1 ? PB1 : PB0;
             constexpr int NM = MA * 4 * N_I, GAP = std::max(1, NM / std::max(1, NF));
             int p = 0;
 #pragma unroll
@@ -274,14 +288,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         // steps [from, to) of pass S while those AHEAD of them, of pass SF, are fetched
         auto steps = [&](int from, int to, auto sc, auto sf) INLINE {
             constexpr int S = decltype(sc)::value, SF = decltype(sf)::value;
-            constexpr int FLY = SF < 0 ? 0 : GRP == 0 ? (AHEAD - 1) * (SF == 0 ? PB0 : PB1) : (SA - 2) * NFA;
+            constexpr int FLY = SF < 0 ? 0 : GRP == 0 ? (AHEAD - 1) * (SF == 1 ? PB1 : PB0) : (SA - 2) * NFA;
             for (int v = from; v < to; ++v) {
                 if (MA > 0) {
                     read(sc, v);
                     // (DX: the first pass may end among steps that still fetch)
-                    if (SF != 0 || OP == GRAD_DX) {
+                    if (SF < 0 || (ACT && SF != S) || OP == GRAD_DX) {
                         const int t = WGT || S == 0 ? (OP == GRAD_DX && v >= nk ? v - nk : v) : v - nk;
-                        if (t == nk - 1 && K % BK) clear_past(K - t * BK);
+                        if (t == nk - 1 && K % BK) clear_others(K - t * BK);
                     }
                 }
                 if (GRP == 1) wait_vm<FLY>();  // A of step v + 1
@@ -293,14 +307,21 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         };
         typedef std::integral_constant<int, 0> s0;
         typedef std::integral_constant<int, 1> s1;
+        typedef std::integral_constant<int, 2> s_last;
         typedef std::integral_constant<int, -1> none;
         const int nv = v_end - v0;
+        const bool ragged = WGT && K % BK;
         constexpr int NF0 = GRP == 1 ? NFA : PB0;
 #pragma unroll
         for (int q = 0; q < AHEAD; ++q)
             if (q < nv) {
+                if (ragged && q == nk - 1) {
 #pragma unroll
-                for (int p = 0; p < NF0; ++p) fill(gc, s0{}, v0 + q, p);
+                    for (int p = 0; p < NF0; ++p) fill(gc, s_last{}, q, p);
+                } else {
+#pragma unroll
+                    for (int p = 0; p < NF0; ++p) fill(gc, s0{}, v0 + q, p);
+                }
             }
         if (nv >= AHEAD) wait_vm<(AHEAD - 1) * NF0>();  // the first step has landed
         else wait_vm<0>();
@@ -313,7 +334,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
             steps(2 * nk - AHEAD, 2 * nk, s1{}, none{});
         } else {
             const int mid = max(v0, v_end - AHEAD);
-            steps(v0, mid, s0{}, s0{});
+            const int whole = ragged ? max(v0, mid - 1) : mid;
+            steps(v0, whole, s0{}, s0{});
+            if constexpr (WGT) steps(whole, mid, s0{}, s_last{});
             steps(mid, v_end, s0{}, none{});
         }
     };
@@ -415,14 +438,62 @@ bool grad_mfma_supported(const GradArgs& g) {
     return d > 2 * BK && F > 2 * BK && P * d * 2 < (1ll << 32) && P * F * 2 < (1ll << 32) && d * F * 2 < (1ll << 32);
 }
 
+// ---- gx in parts --------------------------------------------------------------------------------------
+// Its tiles are few (rows by d, where the other products have F or F by d) and long (2 F deep).  Where they do not fill the CUs their k-steps are cut
+// into up to four runs, summed by a launch of its own in fp32.  A model of the launch in us decides: rounds of 256 workgroups (the last
+// one of halves where that does), 1.15 us a step of full tiles, 0.8 of near empty ones, 8 us beside the steps, and the sums at 4.5 TB/s.
+size_t grad_parts_bytes(long long P, int d) {  // room for them; does not fall as P grows
+    return std::min<size_t>(16 * (size_t)P * d, 200u << 20);
+}
+int grad_parts(const GradArgs& g) {
+    const double groups = std::min(g.P, g.E), m = std::max(groups, g.P / 256.0 + 0.6 * groups), tiles = m * ((g.d + 255) / 256);
+    const double step = std::max(0.8, 1.15 * std::min(1.0, g.P / groups / 192)), steps = 2 * ((g.F + BK - 1) / BK);
+    const int most = (int)std::min<size_t>(4, grad_parts_bytes(g.P, g.d) / (4 * (size_t)g.P * g.d));
+    int best = 1;
+    double best_cost = 0;
+    for (int q = 1; q <= most && steps / q >= 8; ++q) {
+        double rounds = tiles * q / 256;
+        rounds = rounds <= 1 ? 1 : std::ceil(2 * rounds) / 2;
+        const double cost = rounds * (steps / q * step + 8) + (q > 1 ? 6 + 4.0 * q * g.P * g.d / 4.5e6 : 0);
+        if (q == 1 || cost < best_cost) best = q, best_cost = cost;
+    }
+    return best;
+}
+
+// gx = the sum of its parts, in order, rounded once; rows of no group stay as they are
+__global__ __launch_bounds__(256) void sum_grad_parts_kernel(const float* __restrict__ parts, int q, const int32_t* __restrict__ offsets, int E, int P, int d,
+                                                             bf16_t* __restrict__ gx) {
+    const long long n = (long long)min(max(offsets[E], 0), P) * d, all = (long long)P * d;
+    for (long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 8; i < n; i += (long long)gridDim.x * (256 * 8)) {
+        f32x4 lo{}, hi{};
+        for (int p = 0; p < q; ++p) {
+            lo += *reinterpret_cast<const f32x4*>(parts + p * all + i);
+            hi += *reinterpret_cast<const f32x4*>(parts + p * all + i + 4);
+        }
+        bf16x8 o;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] = (bf16_t)lo[j], o[4 + j] = (bf16_t)hi[j];
+        *reinterpret_cast<bf16x8*>(gx + i) = o;
+    }
+}
+
 int run_grad_mfma(const GradArgs& g, GradOp op, hipStream_t st) {
     if (op == GRAD_WEIGHTS) {
         const int strips = g.E * 3 * ((g.F + 255) / 256);
         return launch<GRAD_WEIGHTS, false>(g, (strips + 7) / 8 * 8 * ((g.d + 255) / 256), st);
     }
     const int m = m_tiles_bound(g.P, g.E, BM);
-    if (op == GRAD_ACT) return launch<GRAD_ACT, false>(g, find_tile_grid(m * ((g.F + Form<GRAD_ACT>::BN - 1) / Form<GRAD_ACT>::BN), 0), st);
-    return launch<GRAD_DX, false>(g, find_tile_grid(m * ((g.d + 255) / 256), 0), st);
+    if (op == GRAD_ACT) return launch<GRAD_ACT, false>(g, find_tile_grid(m * ((g.F + Form<GRAD_ACT>::BN - 1) / Form<GRAD_ACT>::BN), kSplitSlots), st);
+    const int tiles = m * ((g.d + 255) / 256), parts = grad_parts(g);
+    if (parts == 1) return launch<GRAD_DX, false>(g, find_tile_grid(tiles, kSplitSlots), st);
+    GradArgs cut = g;
+    cut.k_parts = parts;
+    const int rc = launch<GRAD_DX, true>(cut, find_tile_grid(tiles * parts, kSplitSlots), st);
+    if (rc != MOE_OK) return rc;
+    const long long chunks = (long long)g.P * g.d / 8;
+    hipLaunchKernelGGL(sum_grad_parts_kernel, dim3((unsigned)std::min<long long>((chunks + 255) / 256, 2048)), dim3(256), 0, st, g.parts, parts, g.offsets, g.E,
+                       g.P, g.d, static_cast<bf16_t*>(g.gx));
+    return launch_status();
 }
 
 }  // namespace moe
