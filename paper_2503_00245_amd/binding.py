@@ -510,74 +510,83 @@ def _workspace(workspace: Optional[torch.Tensor], device: int):
     return _ptr(workspace)
 
 
+def _stream_on(device: int) -> int:
+    """_stream of a device's index (-1: host tensors, which no launch is reached with)"""
+    return _raw_stream(device) if _raw_stream is not None and device >= 0 else torch.cuda.current_stream().cuda_stream if device >= 0 else 0
+
+
 def _layer_sizes(shape: MoeShape):
-    """Shapes of tokens, rows, picks and pairs, and the type of rows"""
+    """Shapes of tokens, rows and picks, and the type of rows"""
     T, d, k = shape.n_tokens, shape.d_model, shape.top_k
-    return (T, d), (T * k, d), (T, k), (T * k,), _DTYPES.get(shape.act_dtype)
+    return (T, d), (T * k, d), (T, k), _DTYPES.get(shape.act_dtype)
 
 
-def _pairs_arg(name: str, t, dtype, shape: MoeShape, device: int):
-    """Pointer of a value for each pair, [T,k] or [T k]"""
-    picks, pairs = (shape.n_tokens, shape.top_k), (shape.n_tokens * shape.top_k,)
-    return _arg(name, t, dtype, pairs if t is not None and t.dim() == 1 else picks, device)
+def _rows_of_pairs(t: torch.Tensor, picks, device: int):
+    """Pointer of inv_perm, [T k] or [T,k]"""
+    return _arg("inv_perm", t, torch.int32, (picks[0] * picks[1],) if t.dim() == 1 else picks, device)
 
 
 def moe_dispatch(shape: MoeShape, topk_idx, weight, x, expert_offsets, perm, inv_perm, x_perm, workspace=None) -> None:
     """topk_idx int32 [T,k], weight f32 [T,k] or None, x [T,d]; expert_offsets int32 [E+1], perm and inv_perm int32 [T k],
     x_perm [T k,d]: outputs."""
-    tokens, rows, picks, pairs, dtype = _layer_sizes(shape)
-    at, i32 = x.get_device(), torch.int32
-    _check("moe_dispatch", lib().moe_dispatch(
+    tokens, rows, picks, dtype = _layer_sizes(shape)
+    at, i32, pairs = x.get_device(), torch.int32, rows[:1]
+    status = lib().moe_dispatch(
         C.byref(shape), _arg("topk_idx", topk_idx, i32, picks, at), _arg("weight", weight, torch.float32, picks, at), _arg("x", x, dtype, tokens, at),
         _arg("expert_offsets", expert_offsets, i32, (shape.n_experts + 1,), at), _arg("perm", perm, i32, pairs, at),
-        _pairs_arg("inv_perm", inv_perm, i32, shape, at), _arg("x_perm", x_perm, dtype, rows, at), _workspace(workspace, at), _bytes(workspace),
-        _stream(x.device)))
+        _rows_of_pairs(inv_perm, picks, at), _arg("x_perm", x_perm, dtype, rows, at), _workspace(workspace, at), _bytes(workspace), _stream_on(at))
+    if status:
+        raise MoeError("moe_dispatch", status)
 
 
 def moe_dispatch_backward(shape: MoeShape, grad_x_perm, inv_perm, x, weight, grad_x, grad_weight=None) -> None:
     """grad_x_perm [T k,d], inv_perm int32 [T k] or [T,k], x [T,d] or None without grad_weight, weight f32 [T,k] or None; grad_x [T,d]
     and grad_weight f32 [T,k] (or None): outputs."""
-    tokens, rows, picks, _, dtype = _layer_sizes(shape)
+    tokens, rows, picks, dtype = _layer_sizes(shape)
     at, f32 = grad_x_perm.get_device(), torch.float32
-    _check("moe_dispatch_backward", lib().moe_dispatch_backward(
-        C.byref(shape), _arg("grad_x_perm", grad_x_perm, dtype, rows, at), _pairs_arg("inv_perm", inv_perm, torch.int32, shape, at),
-        _arg("x", x, dtype, tokens, at), _arg("weight", weight, f32, picks, at), _arg("grad_x", grad_x, dtype, tokens, at),
-        _arg("grad_weight", grad_weight, f32, picks, at), _stream(grad_x_perm.device)))
+    status = lib().moe_dispatch_backward(
+        C.byref(shape), _arg("grad_x_perm", grad_x_perm, dtype, rows, at), _rows_of_pairs(inv_perm, picks, at), _arg("x", x, dtype, tokens, at),
+        _arg("weight", weight, f32, picks, at), _arg("grad_x", grad_x, dtype, tokens, at), _arg("grad_weight", grad_weight, f32, picks, at), _stream_on(at))
+    if status:
+        raise MoeError("moe_dispatch_backward", status)
 
 
 def moe_collect(shape: MoeShape, y_perm, inv_perm, topk_gate, residual, y) -> None:
     """y_perm [T k,d], inv_perm int32 [T k] or [T,k], topk_gate f32 [T,k], residual [T,d] or None; y [T,d]: output."""
-    tokens, rows, picks, _, dtype = _layer_sizes(shape)
+    tokens, rows, picks, dtype = _layer_sizes(shape)
     at = y_perm.get_device()
-    _check("moe_collect", lib().moe_collect(
-        C.byref(shape), _arg("y_perm", y_perm, dtype, rows, at), _pairs_arg("inv_perm", inv_perm, torch.int32, shape, at),
-        _arg("topk_gate", topk_gate, torch.float32, picks, at), _arg("residual", residual, dtype, tokens, at), _arg("y", y, dtype, tokens, at),
-        _stream(y_perm.device)))
+    status = lib().moe_collect(
+        C.byref(shape), _arg("y_perm", y_perm, dtype, rows, at), _rows_of_pairs(inv_perm, picks, at), _arg("topk_gate", topk_gate, torch.float32, picks, at),
+        _arg("residual", residual, dtype, tokens, at), _arg("y", y, dtype, tokens, at), _stream_on(at))
+    if status:
+        raise MoeError("moe_collect", status)
 
 
 def moe_collect_backward(shape: MoeShape, grad_y, y_perm, expert_offsets, inv_perm, topk_gate, grad_y_perm=None, grad_gate=None) -> None:
     """grad_y [T,d], y_perm [T k,d] or None without grad_gate, expert_offsets int32 [E+1], inv_perm int32 [T k] or [T,k], topk_gate
     f32 [T,k]; grad_y_perm [T k,d] and grad_gate f32 [T,k], either or None: outputs."""
-    tokens, rows, picks, _, dtype = _layer_sizes(shape)
+    tokens, rows, picks, dtype = _layer_sizes(shape)
     at, f32 = grad_y.get_device(), torch.float32
-    _check("moe_collect_backward", lib().moe_collect_backward(
+    status = lib().moe_collect_backward(
         C.byref(shape), _arg("grad_y", grad_y, dtype, tokens, at), _arg("y_perm", y_perm, dtype, rows, at),
-        _arg("expert_offsets", expert_offsets, torch.int32, (shape.n_experts + 1,), at), _pairs_arg("inv_perm", inv_perm, torch.int32, shape, at),
-        _arg("topk_gate", topk_gate, f32, picks, at), _arg("grad_y_perm", grad_y_perm, dtype, rows, at),
-        _arg("grad_gate", grad_gate, f32, picks, at), _stream(grad_y.device)))
+        _arg("expert_offsets", expert_offsets, torch.int32, (shape.n_experts + 1,), at), _rows_of_pairs(inv_perm, picks, at),
+        _arg("topk_gate", topk_gate, f32, picks, at), _arg("grad_y_perm", grad_y_perm, dtype, rows, at), _arg("grad_gate", grad_gate, f32, picks, at),
+        _stream_on(at))
+    if status:
+        raise MoeError("moe_collect_backward", status)
 
 
 def moe_expert_ffn_backward(shape: MoeShape, weights: MoeWeights, x_perm, expert_offsets, grad_y_perm, grad_x_perm=None, grad_w_gate=None,
                             grad_w_up=None, grad_w_down=None, workspace=None) -> None:
     """x_perm, grad_y_perm [T k,d], expert_offsets int32 [E+1]; grad_x_perm [T k,d], grad_w_gate and grad_w_up [E,F,d], grad_w_down
     [E,d,F], each of them or None: outputs."""
-    _, rows, _, _, dtype = _layer_sizes(shape)
+    _, rows, _, dtype = _layer_sizes(shape)
     E, d, F, at = shape.n_experts, shape.d_model, shape.d_ff, x_perm.get_device()
     _check("moe_expert_ffn_backward", lib().moe_expert_ffn_backward(
         C.byref(shape), C.byref(weights), _arg("x_perm", x_perm, dtype, rows, at), _arg("expert_offsets", expert_offsets, torch.int32, (E + 1,), at),
         _arg("grad_y_perm", grad_y_perm, dtype, rows, at), _arg("grad_x_perm", grad_x_perm, dtype, rows, at),
         _arg("grad_w_gate", grad_w_gate, dtype, (E, F, d), at), _arg("grad_w_up", grad_w_up, dtype, (E, F, d), at),
-        _arg("grad_w_down", grad_w_down, dtype, (E, d, F), at), _workspace(workspace, at), _bytes(workspace), _stream(x_perm.device)))
+        _arg("grad_w_down", grad_w_down, dtype, (E, d, F), at), _workspace(workspace, at), _bytes(workspace), _stream_on(at)))
 
 
 class Block:
@@ -585,6 +594,7 @@ class Block:
 
     def __init__(self, struct: BlockStruct, tensors: Dict[str, Optional[torch.Tensor]]):
         self.struct, self.tensors = struct, tensors
+        self.held = [(name, t) for name, t in tensors.items() if t is not None]
 
 
 def make_block(eps=1e-5, skip_scale=1.0, block_scale=1.0, dropout=0.0, post_w=None, gate=None, token_gate=None, rng=None) -> Block:
@@ -610,13 +620,11 @@ def alloc_block_workspace(n_tokens: int, d_model: int, device) -> torch.Tensor:
 
 
 def _block_check(block: Block, T: int, d: int, device: int, weights: bool) -> None:
-    for name, n in (("post_w", d), ("gate", d), ("token_gate", T)) if weights else ():
-        v = block.tensors[name]
-        if v is not None and v.shape[0] != n:
-            raise ValueError(f"{name} must have {n} values, got {v.shape[0]}")
-    for v in block.tensors.values():
-        if v is not None and v.get_device() != device:
-            raise ValueError("the block's tensors on another device than the call's first tensor")
+    for name, v in block.held:
+        if weights and name != "rng" and v.shape[0] != (T if name == "token_gate" else d):
+            raise ValueError(f"{name} must have {T if name == 'token_gate' else d} values, got {v.shape[0]}")
+        if v.get_device() != device:
+            raise ValueError(f"the block's {name} on another device than the call's first tensor")
 
 
 def moe_block_norm(block: Block, x, b, open_w, y, n) -> None:
@@ -624,9 +632,11 @@ def moe_block_norm(block: Block, x, b, open_w, y, n) -> None:
     T, d = rows = x.shape
     at, dtype = x.get_device(), x.dtype
     _block_check(block, T, d, at, b is not None)
-    _check("moe_block_norm", lib().moe_block_norm(
-        C.byref(block.struct), T, d, _act_dtype(x), _arg("x", x, dtype, rows, at), _arg("b", b, dtype, rows, at),
-        _arg("open_w", open_w, torch.float32, (d,), at), _arg("y", y, dtype, rows, at), _arg("n", n, dtype, rows, at), _stream(x.device)))
+    status = lib().moe_block_norm(
+        C.byref(block.struct), T, d, _act_dtype(x), _ptr(x), _arg("b", b, dtype, rows, at), _arg("open_w", open_w, torch.float32, (d,), at),
+        _arg("y", y, dtype, rows, at), _arg("n", n, dtype, rows, at), _stream_on(at))
+    if status:
+        raise MoeError("moe_block_norm", status)
 
 
 def moe_block_norm_backward(block: Block, grad_y, grad_n, y, b, open_w, grad_x, grad_b=None, grad_open_w=None, grad_post_w=None, grad_gate=None,
@@ -636,12 +646,14 @@ def moe_block_norm_backward(block: Block, grad_y, grad_n, y, b, open_w, grad_x, 
     T, d = rows = grad_x.shape
     at, dtype, f32 = grad_x.get_device(), grad_x.dtype, torch.float32
     _block_check(block, T, d, at, b is not None)
-    _check("moe_block_norm_backward", lib().moe_block_norm_backward(
+    status = lib().moe_block_norm_backward(
         C.byref(block.struct), T, d, _act_dtype(grad_x), _arg("grad_y", grad_y, dtype, rows, at), _arg("grad_n", grad_n, dtype, rows, at),
-        _arg("y", y, dtype, rows, at), _arg("b", b, dtype, rows, at), _arg("open_w", open_w, f32, (d,), at), _arg("grad_x", grad_x, dtype, rows, at),
+        _arg("y", y, dtype, rows, at), _arg("b", b, dtype, rows, at), _arg("open_w", open_w, f32, (d,), at), _ptr(grad_x),
         _arg("grad_b", grad_b, dtype, rows, at), _arg("grad_open_w", grad_open_w, f32, (d,), at), _arg("grad_post_w", grad_post_w, f32, (d,), at),
         _arg("grad_gate", grad_gate, f32, (d,), at), _arg("grad_token_gate", grad_token_gate, f32, (T,), at), _workspace(workspace, at),
-        _bytes(workspace), _stream(grad_x.device)))
+        _bytes(workspace), _stream_on(at))
+    if status:
+        raise MoeError("moe_block_norm_backward", status)
 
 
 def moe_block_stack_workspace_bytes(shape: MoeShape) -> int:
@@ -668,4 +680,4 @@ def moe_block_stack_forward(shape: MoeShape, layers: Sequence[MoeWeights], block
         C.byref(shape), (MoeWeights * n)(*layers), (BlockStruct * n)(*(b.struct for b in blocks)),
         (C.c_void_p * n)(*(_arg("open_w", w, torch.float32, (d,), at) for w in open_w)), n, _arg("x", x, dtype, (T, d), at),
         _arg("y", y, dtype, (T, d), at), _arg("topk_trace", topk_trace, torch.int32, (n, T, shape.top_k), at), _workspace(workspace, at),
-        _bytes(workspace), _stream(x.device)))
+        _bytes(workspace), _stream_on(at)))

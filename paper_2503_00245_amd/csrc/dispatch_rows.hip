@@ -52,10 +52,14 @@ __global__ __launch_bounds__(kThreads) void dispatch_count_kernel(const int32_t*
 // One workgroup a chunk: where its pairs go, then their rows.  A pair's row is its group's start, the group's pairs of earlier
 // chunks, and those before it in the chunk; the last by ballots, so that order by pair is kept.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void dispatch_kernel(const int32_t* __restrict__ keys, const float* __restrict__ weight,
-                                                            const T* __restrict__ x, const int32_t* __restrict__ counts, int n_tokens, int E, int k, int d,
-                                                            int chunk_tokens, int32_t* __restrict__ offsets, int32_t* __restrict__ perm,
-                                                            int32_t* __restrict__ inv_perm, T* __restrict__ x_perm) {
+__global__ __launch_bounds__(kThreads) void dispatch_kernel(ptr_arg a_keys, ptr_arg a_counts, int n_tokens, int E, int k, int d, int chunk_tokens, ptr_arg a_x,
+                                                            ptr_arg a_weight, ptr_arg a_offsets, ptr_arg a_perm, ptr_arg a_inv, ptr_arg a_rows) {
+    const int32_t *const __restrict__ keys = from_arg<const int32_t>(a_keys), *const __restrict__ counts = from_arg<const int32_t>(a_counts);
+    const float* const __restrict__ weight = from_arg<const float>(a_weight);
+    const T* const __restrict__ x = from_arg<const T>(a_x);
+    T* const __restrict__ x_perm = from_arg<T>(a_rows);
+    int32_t *const __restrict__ offsets = from_arg<int32_t>(a_offsets), *const __restrict__ perm = from_arg<int32_t>(a_perm),
+                               *const __restrict__ inv_perm = from_arg<int32_t>(a_inv);
     __shared__ int s_all[kMaxExperts + 1], s_run[kMaxExperts + 1];  // of each expert: pairs, the next row
     __shared__ int s_wave[kWaves][kMaxExperts + 1];
     __shared__ int s_row[kThreads];
@@ -209,9 +213,14 @@ struct Dots {
 
 // out[t] = sum_j w[t,j] rows[inv[t,j]] (+ residual[t]); dots[t,j] = <x[t], rows[inv[t,j]]>
 template <typename T, int WAVES, int K, bool DOTS>
-__global__ __launch_bounds__(256) void collect_kernel(const T* __restrict__ rows, const int32_t* __restrict__ inv_perm, const float* __restrict__ weight,
-                                                      const T* __restrict__ residual, const T* __restrict__ x, int n_tokens, int k, int d, int P,
-                                                      T* __restrict__ out, float* __restrict__ dots) {
+__global__ __launch_bounds__(256) void collect_kernel(ptr_arg a_inv, ptr_arg a_weight, ptr_arg a_rows, int n_tokens, int k, int d, int P, ptr_arg a_residual,
+                                                      ptr_arg a_x, ptr_arg a_out, ptr_arg a_dots) {
+    const T *const __restrict__ rows = from_arg<const T>(a_rows), *const __restrict__ residual = from_arg<const T>(a_residual),
+                               *const __restrict__ x = from_arg<const T>(a_x);
+    const int32_t* const __restrict__ inv_perm = from_arg<const int32_t>(a_inv);
+    const float* const __restrict__ weight = from_arg<const float>(a_weight);
+    T* const __restrict__ out = from_arg<T>(a_out);
+    float* const __restrict__ dots = from_arg<float>(a_dots);
     extern __shared__ float s_dots[];
     __shared__ float s_part[4][kWave];
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
@@ -272,9 +281,14 @@ __global__ __launch_bounds__(256) void collect_kernel(const T* __restrict__ rows
 
 // grad_rows[inv[t,j]] = gate[t,j] gy[t]; dots[t,j] = <gy[t], rows[inv[t,j]]>.  Rows of no pair are cleared by all workgroups together.
 template <typename T, int WAVES, int K, bool DOTS, bool ROWS>
-__global__ __launch_bounds__(256) void spread_kernel(const T* __restrict__ gy, const T* rows, const int32_t* __restrict__ inv_perm,
-                                                     const float* __restrict__ gate, const int32_t* __restrict__ offsets, int n_tokens, int E, int k, int d,
-                                                     int P, T* grad_rows, float* __restrict__ dots) {
+__global__ __launch_bounds__(256) void spread_kernel(ptr_arg a_inv, ptr_arg a_gate, ptr_arg a_gy, int n_tokens, int E, int k, int d, int P, ptr_arg a_rows,
+                                                     ptr_arg a_offsets, ptr_arg a_grad, ptr_arg a_dots) {
+    const T* const __restrict__ gy = from_arg<const T>(a_gy);
+    const T* const rows = from_arg<const T>(a_rows);  // (may be the output)
+    T* const grad_rows = from_arg<T>(a_grad);
+    const int32_t *const __restrict__ inv_perm = from_arg<const int32_t>(a_inv), *const __restrict__ offsets = from_arg<const int32_t>(a_offsets);
+    const float* const __restrict__ gate = from_arg<const float>(a_gate);
+    float* const __restrict__ dots = from_arg<float>(a_dots);
     extern __shared__ float s_dots[];
     __shared__ float s_part[4][kWave];
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
@@ -360,8 +374,8 @@ int run_collect(const moe_shape& s, const void* rows, const int32_t* inv, const 
         const auto kern = dots ? collect_kernel<T, W, K, true> : collect_kernel<T, W, K, false>;
         static std::atomic<uint64_t> lds_allowed;
         if (lds && allow_dynamic_lds(reinterpret_cast<const void*>(kern), kDotsLds, lds_allowed) != MOE_OK) return (int)MOE_ERR_LAUNCH;
-        hipLaunchKernelGGL(kern, dim3(grid), dim3(256), lds, st, static_cast<const T*>(rows), inv, weight, static_cast<const T*>(residual),
-                           static_cast<const T*>(x), s.n_tokens, s.top_k, s.d_model, s.n_tokens * s.top_k, static_cast<T*>(out), dots);
+        hipLaunchKernelGGL(kern, dim3(grid), dim3(256), lds, st, as_arg(inv), as_arg(weight), as_arg(rows), s.n_tokens, s.top_k, s.d_model,
+                           s.n_tokens * s.top_k, as_arg(residual), as_arg(x), as_arg(out), as_arg(dots));
         return launch_status();
     });
 }
@@ -377,8 +391,8 @@ int run_spread(const moe_shape& s, const void* gy, const void* rows, const int32
         const auto kern = !grad_rows ? spread_kernel<T, W, K, true, false> : dots ? spread_kernel<T, W, K, true, true> : spread_kernel<T, W, K, false, true>;
         static std::atomic<uint64_t> lds_allowed[2];
         if (lds && allow_dynamic_lds(reinterpret_cast<const void*>(kern), kDotsLds, lds_allowed[grad_rows != nullptr]) != MOE_OK) return (int)MOE_ERR_LAUNCH;
-        hipLaunchKernelGGL(kern, dim3(grid), dim3(256), lds, st, static_cast<const T*>(gy), static_cast<const T*>(rows), inv, gate, offsets, s.n_tokens,
-                           s.n_experts, s.top_k, s.d_model, P, static_cast<T*>(grad_rows), dots);
+        hipLaunchKernelGGL(kern, dim3(grid), dim3(256), lds, st, as_arg(inv), as_arg(gate), as_arg(gy), s.n_tokens, s.n_experts, s.top_k, s.d_model, P,
+                           as_arg(rows), as_arg(offsets), as_arg(grad_rows), as_arg(dots));
         return launch_status();
     });
 }
@@ -422,12 +436,9 @@ extern "C" int moe_dispatch(const moe_shape* shape, const int32_t* topk_idx, con
         if ((rc = launch_status()) != MOE_OK) return rc;
     }
     const int grid = std::max(plan.chunks, 1);
-    if (s.act_dtype == MOE_F32)
-        hipLaunchKernelGGL(dispatch_kernel<float>, dim3(grid), dim3(kThreads), 0, st, topk_idx, weight, static_cast<const float*>(x), counts, s.n_tokens,
-                           s.n_experts, s.top_k, s.d_model, plan.tokens, expert_offsets, perm, inv_perm, static_cast<float*>(x_perm));
-    else
-        hipLaunchKernelGGL(dispatch_kernel<bf16_t>, dim3(grid), dim3(kThreads), 0, st, topk_idx, weight, static_cast<const bf16_t*>(x), counts, s.n_tokens,
-                           s.n_experts, s.top_k, s.d_model, plan.tokens, expert_offsets, perm, inv_perm, static_cast<bf16_t*>(x_perm));
+    hipLaunchKernelGGL(s.act_dtype == MOE_F32 ? dispatch_kernel<float> : dispatch_kernel<bf16_t>, dim3(grid), dim3(kThreads), 0, st, as_arg(topk_idx),
+                       as_arg(counts), s.n_tokens, s.n_experts, s.top_k, s.d_model, plan.tokens, as_arg(x), as_arg(weight), as_arg(expert_offsets),
+                       as_arg(perm), as_arg(inv_perm), as_arg(x_perm));
     return launch_status();
 }
 

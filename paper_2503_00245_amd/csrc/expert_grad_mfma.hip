@@ -51,9 +51,10 @@ struct Form {
     static constexpr bool ACT = OP == GRAD_ACT, WGT = OP == GRAD_WEIGHTS;
     static constexpr int WAVES_M = ACT ? 4 : 2, WAVES_N = 8 / WAVES_M;
     static constexpr int MB = 8 / WAVES_M;           // 32-row blocks of a wave: wm, wm + WAVES_M, ...
-    static constexpr int BN = ACT ? 96 : 256;        // output columns
-    static constexpr int NI = ACT ? 6 : 4;           // 16-column blocks of a wave (ACT: three of a, three of b, then three of dh)
-    static constexpr int SA = 2, SB = ACT ? 4 : 3;   // k-steps in LDS
+    static constexpr int BN = ACT ? 128 : 256;       // output columns
+    static constexpr int NI = ACT ? 8 : 4;           // 16-column blocks of a wave (ACT: four of a, four of b, then four of dh)
+    static constexpr int SA = 2, SB = 3;             // k-steps in LDS
+    static constexpr int KS = ACT ? 2 : 1;           // phases that a k-step is multiplied in
     static constexpr int A_BYTES = BM * BK * 2, B_BYTES = ACT ? 2 * BN * BK * 2 : BN * BK * 2;
     static constexpr int LDS = SA * A_BYTES + SB * B_BYTES;
     static_assert(LDS <= 160 * 1024, "LDS of a CU");
@@ -77,7 +78,7 @@ template <int OP, bool PARTS>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void grad_kernel(const GradArgs g) {
     typedef Form<OP> F;
     constexpr bool ACT = F::ACT, WGT = F::WGT;
-    constexpr int WAVES_M = F::WAVES_M, WAVES_N = F::WAVES_N, MB = F::MB, BN = F::BN, NI = F::NI, SA = F::SA, SB = F::SB;
+    constexpr int WAVES_M = F::WAVES_M, WAVES_N = F::WAVES_N, MB = F::MB, BN = F::BN, NI = F::NI, SA = F::SA, SB = F::SB, KS = F::KS;
     constexpr int A_BYTES = F::A_BYTES, B_BYTES = F::B_BYTES, B_AT = SA * A_BYTES;
     extern __shared__ __align__(16) char smem[];
     const int lane = threadIdx.x & 63;
@@ -131,7 +132,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     // ---- fills.  Instruction p of wave w % 4 = fw writes the KB 4 p + fw of its operand's step; lane l the l-th 16 bytes of it.
     const unsigned lds0 = (unsigned)(uintptr_t)(lds_char*)smem;
     constexpr int PA = BM / 32;
-    constexpr int PB0 = ACT ? 6 : 8, PB1 = ACT ? 4 : 8;  // of B in the first and in the second pass
+    constexpr int PB0 = 8, PB1 = ACT ? 4 : 8;  // of B in the first and in the second pass
     // rows of 128 bytes: row 8 (4 p + fw) + l / 8, slot l % 8 = chunk ^ (row / 2) % 8
     const int k_row = fw * 8 + (lane >> 3);
     const unsigned k_chunk = ((lane & 7) ^ (((fw & 1) << 2) | (lane >> 4))) * 16;
@@ -149,10 +150,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         for (int p = 0; p < 2; ++p) col[p] = (unsigned)min(m0 + (t_chunk ^ (p << 3)) * 8, M_pitch - 8) * 2;
     } else if (ACT) {
 #pragma unroll
-        for (int p = 0; p < 3; ++p) off[p] = (unsigned)min(n0 + k_row + 32 * p, N - 1) * ((unsigned)K * 2) + k_chunk;
-        // rows of 256 bytes, 12 of their 16 chunks in use: row 4 (4 p + fw) + l / 16
+        for (int p = 0; p < 4; ++p) off[p] = (unsigned)min(n0 + k_row + 32 * p, N - 1) * ((unsigned)K * 2) + k_chunk;
+        // rows of 256 bytes: row 4 (4 p + fw) + l / 16
         const int f = (lane >> 4) | (fw >> 1) << 2;
-        col[0] = (unsigned)min(n0 + min((lane & 15) ^ (f << 1), 11) * 8, N - 8) * 2 + (unsigned)(4 * fw + (lane >> 4)) * pitch_b;
+        col[0] = (unsigned)min(n0 + ((lane & 15) ^ (f << 1)) * 8, N - 8) * 2 + (unsigned)(4 * fw + (lane >> 4)) * pitch_b;
     } else {
 #pragma unroll
         for (int p = 0; p < 2; ++p) col[p] = (unsigned)min(n0 + (t_chunk ^ (p << 3)) * 8, N - 8) * 2;
@@ -170,7 +171,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         if constexpr (GRP == 1 && !WGT) {
             dma16<false>(slot, (second ? A1 : A0) + k0 * 2, off[p]);
         } else if constexpr (GRP == 0 && ACT && S == 0) {
-            dma16<false>(slot, (p < 3 ? B0 : B1) + k0 * 2, off[p % 3]);
+            dma16<false>(slot, (p < 4 ? B0 : B1) + k0 * 2, off[p % 4]);
         } else if constexpr (GRP == 0 && ACT) {
             dma16<false>(slot, B2 + (size_t)(unsigned)(k0 + 16 * p) * pitch_b, col[0]);
         } else {
@@ -185,7 +186,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         }
     };
 
-    f32x4 acc[2 * MB][NI], acc2[ACT ? 2 * MB : 1][ACT ? 3 : 1];
+    f32x4 acc[2 * MB][NI], acc2[ACT ? 2 * MB : 1][ACT ? NI / 2 : 1];
 #pragma unroll
     for (int mi = 0; mi < 2 * MB; ++mi)
 #pragma unroll
@@ -194,14 +195,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
         for (int mi = 0; mi < 2 * MB; ++mi)
 #pragma unroll
-            for (int ni = 0; ni < 3; ++ni) acc2[mi][ni] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int ni = 0; ni < NI / 2; ++ni) acc2[mi][ni] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     const int live = min(MB, max(0, ((min(rows_here, BM) + 31) / 32 + WAVES_M - 1 - wm) / WAVES_M));
 
     // ---- fragment reads.  Rows of 128 bytes: row l % 16 of a block, chunk 4 ks + l / 16.
     const unsigned c16 = ((lane >> 4) ^ ((lane & 15) >> 1)) << 4;
     const unsigned ra = lds0 + wm * 4096 + (lane & 15) * 128 + c16;
-    const unsigned rb = lds0 + B_AT + wn * 48 * 128 + (lane & 15) * 128 + c16;  // (ACT, first pass)
+    const unsigned rb = lds0 + B_AT + wn * 64 * 128 + (lane & 15) * 128 + c16;  // (ACT, first pass)
     // rows read transposed: row 8 (l / 16) + (l % 16) / 4 (+ 4) of a 32-row half step, 8 bytes (l % 4) of unit u ^ f
     constexpr int T_ROW = ACT ? 256 : 512;
     const unsigned t_swz = (((lane & 15) >> 2) | ((lane >> 4) & 1) << 2) << 5;
@@ -211,9 +212,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         constexpr int MA = decltype(ma)::value, GRP = decltype(gc)::value, MR = MA > 0 ? MA : 1;
         constexpr int NFA = WGT || MA == MB ? PA : std::min(PA, WAVES_M * (MA + 1) - 1);
         constexpr int AHEAD = GRP == 0 ? SB - 1 : SA;
-        bf16x8 fa[2][2 * MR], fb[2][NI];
-        auto read = [&](auto sc, int v) INLINE {
-            constexpr int S = decltype(sc)::value, N_I = ACT && S == 1 ? 3 : NI;
+        constexpr int HS = 2 / KS;  // half steps (32 k-values) of a phase
+        bf16x8 fa[HS][2 * MR], fb[HS][NI];
+        auto read = [&](auto sc, int v, int phase) INLINE {
+            constexpr int S = decltype(sc)::value, N_I = ACT && S == 1 ? NI / 2 : NI;
             const unsigned pa = v % SA * A_BYTES, pb = v % SB * B_BYTES;
             // (an address for each unit is made here, of two instructions; kept over the loop, they did not fit the registers)
             unsigned swz = t_swz;
@@ -221,61 +223,63 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
             if (!ACT || S == 1) asm volatile("" : "+v"(swz));
 #endif
 #pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
+            for (int q = 0; q < HS; ++q) {
+                const int ks = KS == 2 ? phase : q;
 #pragma unroll
                 for (int ni = 0; ni < N_I; ++ni) {
                     if constexpr (ACT && S == 0) {
-                        fb[ks][ni] = *reinterpret_cast<const __attribute__((address_space(3))) bf16x8*>(
-                            (uintptr_t)((rb ^ (ks << 6)) + pb + (ni / 3) * (96 * 128) + (ni % 3) * 2048));
+                        fb[q][ni] = *reinterpret_cast<const __attribute__((address_space(3))) bf16x8*>(
+                            (uintptr_t)((rb ^ (ks << 6)) + pb + (ni / 4) * (128 * 128) + (ni % 4) * 2048));
                     } else if constexpr (ACT) {
-                        const unsigned unit = (unsigned)(wn * 3 + ni) << 5;
-                        fb[ks][ni] = read_transposed((unit ^ swz) + (t_lane + B_AT + pb) + ks * (32 * T_ROW), 4 * T_ROW);
+                        const unsigned unit = (unsigned)(wn * 4 + ni) << 5;
+                        fb[q][ni] = read_transposed((unit ^ swz) + (t_lane + B_AT + pb) + ks * (32 * T_ROW), 4 * T_ROW);
                     } else {
                         const unsigned unit = (unsigned)(wn * NI + ni) << 5;
-                        fb[ks][ni] = read_transposed((unit ^ swz) + (t_lane + B_AT + pb) + ks * (32 * T_ROW), 4 * T_ROW);
+                        fb[q][ni] = read_transposed((unit ^ swz) + (t_lane + B_AT + pb) + ks * (32 * T_ROW), 4 * T_ROW);
                     }
                 }
 #pragma unroll
                 for (int mi = 0; mi < 2 * MA; ++mi) {
                     if constexpr (WGT) {
                         const unsigned unit = (unsigned)((wm + (mi >> 1) * WAVES_M) * 2 + (mi & 1)) << 5;
-                        fa[ks][mi] = read_transposed((unit ^ swz) + (t_lane + pa) + ks * (32 * T_ROW), 4 * T_ROW);
+                        fa[q][mi] = read_transposed((unit ^ swz) + (t_lane + pa) + ks * (32 * T_ROW), 4 * T_ROW);
                     } else {
-                        fa[ks][mi] = *reinterpret_cast<const __attribute__((address_space(3))) bf16x8*>(
+                        fa[q][mi] = *reinterpret_cast<const __attribute__((address_space(3))) bf16x8*>(
                             (uintptr_t)((ra ^ (ks << 6)) + pa + (mi >> 1) * (WAVES_M * 4096) + (mi & 1) * 2048));
                     }
                 }
             }
         };
         // the last step of a pass, `left` k-values of which are its own: the others are taken out of A
-        auto clear_others = [&](int left) INLINE {
+        auto clear_others = [&](int left, int phase) INLINE {
 #pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
+            for (int q = 0; q < HS; ++q) {
+                const int ks = KS == 2 ? phase : q;
                 if constexpr (WGT) {  // they are the last ones
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         const bool past = ks * 32 + (lane >> 4) * 8 + j >= left;
 #pragma unroll
-                        for (int mi = 0; mi < 2 * MA; ++mi) fa[ks][mi][j] = past ? (bf16_t)0.f : fa[ks][mi][j];
+                        for (int mi = 0; mi < 2 * MA; ++mi) fa[q][mi][j] = past ? (bf16_t)0.f : fa[q][mi][j];
                     }
                 } else if (ks * 32 + (lane >> 4) * 8 < BK - left) {  // they are the first ones (a multiple of 8)
 #pragma unroll
-                    for (int mi = 0; mi < 2 * MA; ++mi) fa[ks][mi] = bf16x8{};
+                    for (int mi = 0; mi < 2 * MA; ++mi) fa[q][mi] = bf16x8{};
                 }
             }
         };
-        // products of a step of pass S, between them the fills of step vf of pass SF (< 0: none)
-        auto multiply = [&](auto sc, auto sf, int vf) INLINE {
-            constexpr int S = decltype(sc)::value, SF = decltype(sf)::value, N_I = ACT && S == 1 ? 3 : NI;
-            constexpr int NF = SF < 0 ? 0 : GRP == 1 ? NFA : SF == 1 ? PB1 : PB0;
-            constexpr int NM = MA * 4 * N_I, GAP = std::max(1, NM / std::max(1, NF));
-            int p = 0;
+        // products of a phase of pass S, between them fills [p, p_end) of step vf of pass SF
+        auto multiply = [&](auto sc, auto sf, auto pc, auto pn, int vf) INLINE {
+            constexpr int S = decltype(sc)::value, N_I = ACT && S == 1 ? NI / 2 : NI;
+            constexpr int P0 = decltype(pc)::value, P_END = decltype(pn)::value, NF = P_END - P0;
+            constexpr int NM = MA * 2 * HS * N_I, GAP = std::max(1, NM / std::max(1, NF));
+            int p = P0;
 #pragma unroll
             for (int i = 0; i < NM; ++i) {
-                const int ni = i % N_I, mi = i / N_I % (2 * MR), ks = i / (N_I * 2 * MR);
+                const int ni = i % N_I, mi = i / N_I % (2 * MR), q = i / (N_I * 2 * MR);
                 f32x4& c = ACT && S == 1 ? acc2[ACT ? mi : 0][ACT ? ni : 0] : acc[mi][ni];
-                c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[ks][ni], fa[ks][mi], c, 0, 0, 0);
-                if (i % GAP == GAP - 1 && p < NF) {
+                c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[q][ni], fa[q][mi], c, 0, 0, 0);
+                if (i % GAP == GAP - 1 && p < P_END) {
                     __builtin_amdgcn_sched_barrier(0);
                     fill(gc, sf, vf, p);
                     ++p;
@@ -283,26 +287,32 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                 }
             }
 #pragma unroll
-            for (; p < NF; ++p) fill(gc, sf, vf, p);
+            for (; p < P_END; ++p) fill(gc, sf, vf, p);
         };
         // steps [from, to) of pass S while those AHEAD of them, of pass SF, are fetched
         auto steps = [&](int from, int to, auto sc, auto sf) INLINE {
             constexpr int S = decltype(sc)::value, SF = decltype(sf)::value;
-            constexpr int FLY = SF < 0 ? 0 : GRP == 0 ? (AHEAD - 1) * (SF == 1 ? PB1 : PB0) : (SA - 2) * NFA;
+            constexpr int NF = SF < 0 ? 0 : GRP == 1 ? NFA : SF == 1 ? PB1 : PB0;
+            constexpr int FLY = SF < 0 ? 0 : GRP == 0 ? (AHEAD - 1) * NF : (SA - 2) * NFA;
             for (int v = from; v < to; ++v) {
-                if (MA > 0) {
-                    read(sc, v);
-                    // (DX: the first pass may end among steps that still fetch)
-                    if (SF < 0 || (ACT && SF != S) || OP == GRAD_DX) {
-                        const int t = WGT || S == 0 ? (OP == GRAD_DX && v >= nk ? v - nk : v) : v - nk;
-                        if (t == nk - 1 && K % BK) clear_others(K - t * BK);
+                static_for<KS>([&](auto phase) INLINE {
+                    constexpr bool LAST = phase == KS - 1;
+                    if (MA > 0) {
+                        read(sc, v, phase);
+                        // (DX: the first pass may end among steps that still fetch)
+                        if (SF < 0 || (ACT && SF != S) || OP == GRAD_DX) {
+                            const int t = WGT || S == 0 ? (OP == GRAD_DX && v >= nk ? v - nk : v) : v - nk;
+                            if (t == nk - 1 && K % BK) clear_others(K - t * BK, phase);
+                        }
                     }
-                }
-                if (GRP == 1) wait_vm<FLY>();  // A of step v + 1
-                phase_end();
-                multiply(sc, sf, v + AHEAD);
-                if (GRP == 0) wait_vm<FLY>();  // B of step v + 1
-                phase_end();
+                    if (GRP == 1 && LAST) wait_vm<FLY>();  // A of step v + 1
+                    phase_end();
+                    // A's slot is free once its step's last phase has been read; B's is that of the step before
+                    constexpr int P0 = GRP == 1 ? (LAST ? 0 : NF) : NF * phase / KS, P_END = GRP == 1 ? NF : NF * (phase + 1) / KS;
+                    multiply(sc, sf, std::integral_constant<int, P0>{}, std::integral_constant<int, P_END>{}, v + AHEAD);
+                    if (GRP == 0 && LAST) wait_vm<FLY>();  // B of step v + 1
+                    phase_end();
+                });
             }
         };
         typedef std::integral_constant<int, 0> s0;
@@ -390,17 +400,24 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         if (mb >= live) continue;
         const int rbk = (WAVES_M * mb + wm) * 32;
         if constexpr (ACT) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int nb = 0; nb < NI / 2; ++nb)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const ActGrad v = act_grad(acc[2 * mb + h][nb][j], acc[2 * mb + h][nb + NI / 2][j], acc2[2 * mb + h][nb][j]);
+                        acc[2 * mb + h][nb][j] = v.h, acc[2 * mb + h][nb + NI / 2][j] = v.da, acc2[2 * mb + h][nb][j] = v.db;
+                    }
             static_for<3>([&](auto what) INLINE {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int nb = 0; nb < 3; ++nb) {
+                    for (int nb = 0; nb < NI / 2; ++nb) {
                         bf16x4 o;
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const ActGrad v = act_grad(acc[2 * mb + h][nb][j], acc[2 * mb + h][nb + 3][j], acc2[2 * mb + h][nb][j]);
-                            o[j] = (bf16_t)(what == 0 ? v.h : what == 1 ? v.da : v.db);
-                        }
+                        for (int j = 0; j < 4; ++j)
+                            o[j] = (bf16_t)(what == 0 ? acc[2 * mb + h][nb][j] : what == 1 ? acc[2 * mb + h][nb + NI / 2][j] : acc2[2 * mb + h][nb][j]);
                         *reinterpret_cast<bf16x4*>(wr + h * 16 * PITCH + nb * 32) = o;
                     }
                 leave(rbk, static_cast<bf16_t*>(what == 0 ? g.h : what == 1 ? g.da : g.db) + at0);
