@@ -2,7 +2,7 @@
 // rows, and the gradient of both in one pass and a small sum over tokens (moe_training.h states them).
 //
 // A row is held in registers, so that every tensor is read once and written once: what bounds both is memory.
-// WAVES of a workgroup share a row of up to WAVES * 512 * CHUNKS values; one wave a row where rows fill the chip (no barrier).
+// WAVES of a workgroup share a row of up to WAVES * 512 * CHUNKS values.
 #include <algorithm>
 #include <cmath>
 
@@ -73,95 +73,143 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* s, int& turn) {
     }
 }
 
+// Eight values of a [d] weight for each chunk of a lane.  HOLD: kept over the rows; else read for every row again (rows too wide for
+// that).  Without the weight: ones.
+template <int CHUNKS, bool HOLD>
+struct Columns {
+    const float* w;
+    Raw8<float> v[HOLD ? CHUNKS : 1];
+    __device__ __forceinline__ static Raw8<float> get(const float* w, int c, int d) {
+        Raw8<float> r{};
+        if (w && c < d) return load8(w + c);
+        r.v[0] = r.v[1] = f32x4{1.f, 1.f, 1.f, 1.f};
+        return r;
+    }
+    __device__ __forceinline__ void begin(const float* from, int c0, int step, int d) {
+        w = from;
+        if constexpr (HOLD) {
+#pragma unroll
+            for (int q = 0; q < CHUNKS; ++q) v[q] = get(w, c0 + q * step, d);
+        }
+    }
+    __device__ __forceinline__ Raw8<float> at(int q, int c, int d) const {
+        if constexpr (HOLD) return v[q];
+        else return get(w, c, d);
+    }
+};
+
+// Rows of one tensor that a lane has in hand (zeros where there is none)
+template <typename T, int CHUNKS>
+struct RowPart {
+    Raw8<T> v[CHUNKS];
+    __device__ __forceinline__ void load(const void* from, size_t row, int c0, int step, int d) {
+#pragma unroll
+        for (int q = 0; q < CHUNKS; ++q) {
+            v[q] = Raw8<T>{};
+            if (from && c0 + q * step < d) v[q] = load8(static_cast<const T*>(from) + row + c0 + q * step);
+        }
+    }
+};
+
+// Both kernels: workgroups take rows in turn.  What a lane needs of the [d] weights stays in its registers (up to 8192 values a row: eight
+// a lane), and the next row is on its way while one is summed.
 template <typename T, int WAVES, int CHUNKS>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void block_norm_kernel(const BlockArgs g) {
+    constexpr int ROWS = WAVES == 1 ? 4 : 1, STEP = WAVES * kWave * 8;
+    constexpr bool HOLD = CHUNKS == 1;
     __shared__ float s_sum[2 * 4 * WAVES];
     int turn = 0;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const int t = WAVES == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
+    const int c0 = ((WAVES == 1 ? 0 : wave * kWave) + lane) * 8, stride = gridDim.x * ROWS;
+    int t = blockIdx.x * ROWS + (WAVES == 1 ? wave : 0);
     if (t >= g.T) return;
-    const int c0 = ((WAVES == 1 ? 0 : wave * kWave) + lane) * 8;
-    constexpr int STEP = WAVES * kWave * 8;
-    const T *const x = static_cast<const T*>(g.x) + (size_t)t * g.d, *const b = static_cast<const T*>(g.b) + (size_t)t * g.d;
-    Raw8<T> xv[CHUNKS], bv[CHUNKS];
-#pragma unroll
-    for (int q = 0; q < CHUNKS; ++q) {
-        const int c = c0 + q * STEP;
-        xv[q] = Raw8<T>{}, bv[q] = Raw8<T>{};
-        if (c < g.d) {
-            xv[q] = load8(x + c);
-            if (g.b) bv[q] = load8(b + c);
+    RowPart<T, CHUNKS> x, b;
+    x.load(g.x, (size_t)t * g.d, c0, STEP, g.d);
+    b.load(g.b, (size_t)t * g.d, c0, STEP, g.d);
+    Columns<CHUNKS, HOLD> post_w, gate, open_w;
+    post_w.begin(g.post_w, c0, STEP, g.d);
+    gate.begin(g.gate, c0, STEP, g.d);
+    open_w.begin(g.open_w, c0, STEP, g.d);
+    uint64_t seed = 0, offset = 0;
+    if (g.drop && g.b) seed = g.rng[0], offset = g.rng[1];
+    for (;;) {
+        const size_t row = (size_t)t * g.d;
+        const int next = t + stride;
+        RowPart<T, CHUNKS> x1, b1;
+        if (HOLD && next < g.T) {
+            x1.load(g.x, (size_t)next * g.d, c0, STEP, g.d);
+            b1.load(g.b, (size_t)next * g.d, c0, STEP, g.d);
         }
-    }
-    if (g.b) {
-        float r = 1.f;
-        if (g.post_w) {
+        if (g.b) {
+            float r = 1.f;
+            if (g.post_w) {
+                float sum[1] = {0.f};
+#pragma unroll
+                for (int q = 0; q < CHUNKS; ++q)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) sum[0] = fmaf(at8(b.v[q], i), at8(b.v[q], i), sum[0]);
+                row_sums<WAVES>(sum, s_sum, turn);
+                r = rsqrtf(fmaf(sum[0], g.inv_d, g.eps));
+            }
+            const float scale = g.block_scale * g.keep_scale * (g.token_gate ? g.token_gate[t] : 1.f);
+#pragma unroll
+            for (int q = 0; q < CHUNKS; ++q) {
+                const int c = c0 + q * STEP;
+                if (c >= g.d) continue;
+                const unsigned kept = g.drop ? kept8(seed, offset, (row + c) >> 3, g.drop) : 0xFFu;
+                const Raw8<float> pw = post_w.at(q, c, g.d), gt = gate.at(q, c, g.d);
+                float o[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float z = at8(b.v[q], i) * r * at8(pw, i);
+                    o[i] = fmaf(scale * at8(gt, i), (kept >> i & 1u) ? z : 0.f, g.skip_scale * at8(x.v[q], i));
+                }
+                x.v[q] = round8<T>(o);
+                store8(static_cast<T*>(g.y) + row + c, x.v[q]);
+            }
+        }
+        if (g.open_w) {
             float sum[1] = {0.f};
 #pragma unroll
             for (int q = 0; q < CHUNKS; ++q)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum[0] = fmaf(at8(bv[q], i), at8(bv[q], i), sum[0]);
+                for (int i = 0; i < 8; ++i) sum[0] = fmaf(at8(x.v[q], i), at8(x.v[q], i), sum[0]);
             row_sums<WAVES>(sum, s_sum, turn);
-            r = rsqrtf(fmaf(sum[0], g.inv_d, g.eps));
-        }
-        const float scale = g.block_scale * (g.token_gate ? g.token_gate[t] : 1.f);
-        uint64_t seed = 0, offset = 0;
-        if (g.drop) seed = g.rng[0], offset = g.rng[1];
+            const float r = rsqrtf(fmaf(sum[0], g.inv_d, g.eps));
 #pragma unroll
-        for (int q = 0; q < CHUNKS; ++q) {
-            const int c = c0 + q * STEP;
-            if (c >= g.d) continue;
-            const unsigned kept = g.drop ? kept8(seed, offset, ((uint64_t)t * g.d + c) >> 3, g.drop) : 0xFFu;
-            Raw8<float> pw{}, gt{};
-            if (g.post_w) pw = load8(g.post_w + c);
-            if (g.gate) gt = load8(g.gate + c);
-            float o[8];
+            for (int q = 0; q < CHUNKS; ++q) {
+                const int c = c0 + q * STEP;
+                if (c >= g.d) continue;
+                const Raw8<float> w = open_w.at(q, c, g.d);
+                float o[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float z = at8(bv[q], i);
-                if (g.post_w) z = z * r * at8(pw, i);
-                z = (kept >> i & 1u) ? z * g.keep_scale : 0.f;
-                float m = scale;
-                if (g.gate) m *= at8(gt, i);
-                o[i] = fmaf(m, z, g.skip_scale * at8(xv[q], i));
+                for (int i = 0; i < 8; ++i) o[i] = at8(x.v[q], i) * r * at8(w, i);
+                store8(static_cast<T*>(g.n) + row + c, round8<T>(o));
             }
-            xv[q] = round8<T>(o);
-            store8(static_cast<T*>(g.y) + (size_t)t * g.d + c, xv[q]);
         }
-    }
-    if (!g.open_w) return;
-    float sum[1] = {0.f};
-#pragma unroll
-    for (int q = 0; q < CHUNKS; ++q)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum[0] = fmaf(at8(xv[q], i), at8(xv[q], i), sum[0]);
-    row_sums<WAVES>(sum, s_sum, turn);
-    const float r = rsqrtf(fmaf(sum[0], g.inv_d, g.eps));
-#pragma unroll
-    for (int q = 0; q < CHUNKS; ++q) {
-        const int c = c0 + q * STEP;
-        if (c >= g.d) continue;
-        const Raw8<float> w = load8(g.open_w + c);
-        float o[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = at8(xv[q], i) * r * at8(w, i);
-        store8(static_cast<T*>(g.n) + (size_t)t * g.d + c, round8<T>(o));
+        t = next;
+        if (t >= g.T) return;
+        if (HOLD) {
+            x = x1, b = b1;
+        } else {
+            x.load(g.x, (size_t)t * g.d, c0, STEP, g.d);
+            b.load(g.b, (size_t)t * g.d, c0, STEP, g.d);
+        }
     }
 }
 
 // G = grad_y + r2 (u - y r2^2 mean(u y)), u = grad_n open_w; z = G * (what the norm of b was multiplied by), and for a post_w the
-// same once more: grad_b = r1 (v - b r1^2 mean(v b)), v = z post_w.  A workgroup takes rows in turn and keeps its sums over them for
-// the [d] gradients in registers, a value per column (PARTS); they are added up over the workgroups by a second kernel.
-// ROWS: rows that a workgroup has in hand (one wave each where WAVES is 1).
+// same once more: grad_b = r1 (v - b r1^2 mean(v b)), v = z post_w.  A workgroup keeps its sums over its rows for the [d] gradients in
+// registers, a value per column (PARTS); they are added up over the workgroups by a second kernel.
 template <typename T, int WAVES, int CHUNKS, bool PARTS>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void block_grad_kernel(const BlockArgs g) {
-    constexpr int ROWS = WAVES == 1 ? 4 : 1;
+    constexpr int ROWS = WAVES == 1 ? 4 : 1, STEP = WAVES * kWave * 8;
+    constexpr bool HOLD = CHUNKS == 1;
     __shared__ float s_sum[2 * 4 * WAVES];
     __shared__ float s_parts[PARTS && ROWS > 1 ? ROWS * kWave * 8 : 1];
     int turn = 0;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const int c0 = ((WAVES == 1 ? 0 : wave * kWave) + lane) * 8;
-    constexpr int STEP = WAVES * kWave * 8;
+    const int c0 = ((WAVES == 1 ? 0 : wave * kWave) + lane) * 8, stride = gridDim.x * ROWS;
     float acc[PARTS ? 3 : 1][PARTS ? CHUNKS : 1][8];
     if (PARTS) {
 #pragma unroll
@@ -173,40 +221,40 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void block_grad_k
     }
     uint64_t seed = 0, offset = 0;
     if (g.drop && g.b) seed = g.rng[0], offset = g.rng[1];
-    for (int t = blockIdx.x * ROWS + (WAVES == 1 ? wave : 0); t < g.T; t += gridDim.x * ROWS) {
+    int t = blockIdx.x * ROWS + (WAVES == 1 ? wave : 0);
+    RowPart<T, CHUNKS> gy, gn, y, b;
+    auto fetch = [&](int at) {
+        const size_t row = (size_t)at * g.d;
+        gy.load(g.grad_y, row, c0, STEP, g.d);
+        gn.load(g.grad_n, row, c0, STEP, g.d);
+        y.load(g.grad_n ? g.y : nullptr, row, c0, STEP, g.d);
+        b.load(g.b, row, c0, STEP, g.d);
+    };
+    if (t < g.T) fetch(t);
+    Columns<CHUNKS, HOLD> post_w, gate, open_w;
+    post_w.begin(g.post_w, c0, STEP, g.d);
+    gate.begin(g.gate, c0, STEP, g.d);
+    open_w.begin(g.open_w, c0, STEP, g.d);
+    for (; t < g.T; t += stride) {
         const size_t row = (size_t)t * g.d;
-        Raw8<T> gy[CHUNKS], gn[CHUNKS], y[CHUNKS], b[CHUNKS];
-#pragma unroll
-        for (int q = 0; q < CHUNKS; ++q) {
-            const int c = c0 + q * STEP;
-            gy[q] = gn[q] = y[q] = b[q] = Raw8<T>{};
-            if (c < g.d) {
-                if (g.grad_y) gy[q] = load8(static_cast<const T*>(g.grad_y) + row + c);
-                if (g.grad_n) {
-                    gn[q] = load8(static_cast<const T*>(g.grad_n) + row + c);
-                    y[q] = load8(static_cast<const T*>(g.y) + row + c);
-                }
-                if (g.b) b[q] = load8(static_cast<const T*>(g.b) + row + c);
-            }
-        }
+        const RowPart<T, CHUNKS> gy0 = gy, gn0 = gn, y0 = y, b0 = b;
+        if (HOLD && t + stride < g.T) fetch(t + stride);
         float sum[3] = {0.f, 0.f, 0.f};
 #pragma unroll
         for (int q = 0; q < CHUNKS; ++q) {
-            const int c = c0 + q * STEP;
-            Raw8<float> w{};
-            if (g.grad_n && c < g.d) w = load8(g.open_w + c);
+            const Raw8<float> w = open_w.at(q, c0 + q * STEP, g.d);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float yi = at8(y[q], i), bi = at8(b[q], i);
+                const float yi = at8(y0.v[q], i), bi = at8(b0.v[q], i);
                 sum[0] = fmaf(yi, yi, sum[0]);
-                sum[1] = fmaf(at8(gn[q], i) * at8(w, i), yi, sum[1]);
+                sum[1] = fmaf(at8(gn0.v[q], i) * at8(w, i), yi, sum[1]);
                 sum[2] = fmaf(bi, bi, sum[2]);
             }
         }
-        row_sums<WAVES>(sum, s_sum, turn);
+        if (g.grad_n || g.post_w) row_sums<WAVES>(sum, s_sum, turn);
         const float r2 = rsqrtf(fmaf(sum[0], g.inv_d, g.eps)), r1 = g.post_w ? rsqrtf(fmaf(sum[2], g.inv_d, g.eps)) : 1.f;
         const float m2 = sum[1] * g.inv_d * r2 * r2;
-        const float tg = g.token_gate ? g.token_gate[t] : 1.f;
+        const float tg = g.token_gate ? g.token_gate[t] : 1.f, x_scale = g.b ? g.skip_scale : 1.f;
         float dots[2] = {0.f, 0.f};  // <v, b>; the token gate's gradient
         float v[CHUNKS][8];
 #pragma unroll
@@ -215,56 +263,52 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void block_grad_k
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[q][i] = 0.f;
             if (c >= g.d) continue;
-            float G[8];
+            float G[8], o[8];
+            const Raw8<float> w = open_w.at(q, c, g.d);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) G[i] = at8(gy[q], i);
-            if (g.grad_n) {
-                const Raw8<float> w = load8(g.open_w + c);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float yi = at8(y[q], i), ni = at8(gn[q], i);
+            for (int i = 0; i < 8; ++i) {
+                G[i] = at8(gy0.v[q], i);
+                if (g.grad_n) {
+                    const float yi = at8(y0.v[q], i), ni = at8(gn0.v[q], i);
                     G[i] += r2 * (ni * at8(w, i) - yi * m2);
                     if (PARTS) acc[0][q][i] = fmaf(ni, yi * r2, acc[0][q][i]);
                 }
+                o[i] = x_scale * G[i];
             }
-            float o[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) o[i] = g.b ? g.skip_scale * G[i] : G[i];
             store8(static_cast<T*>(g.grad_x) + row + c, round8<T>(o));
             if (!g.b) continue;
             const unsigned kept = g.drop ? kept8(seed, offset, (row + c) >> 3, g.drop) : 0xFFu;
-            Raw8<float> pw{}, gt{};
-            if (g.post_w) pw = load8(g.post_w + c);
-            if (g.gate) gt = load8(g.gate + c);
+            const Raw8<float> pw = post_w.at(q, c, g.d), gt = gate.at(q, c, g.d);
+            const float scale = g.block_scale * g.keep_scale;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float bi = at8(b[q], i), w = g.post_w ? at8(pw, i) : 1.f, gate = g.gate ? at8(gt, i) : 1.f;
-                const float up = (kept >> i & 1u) ? G[i] * (g.block_scale * g.keep_scale) : 0.f;
-                const float norm = bi * r1;
-                const float bare = (kept >> i & 1u) ? up * (norm * w) : 0.f;  // (a dropped infinity has no part)
-                dots[1] = fmaf(bare, gate, dots[1]);
-                const float z = up * (tg * gate);
+                const bool on = kept >> i & 1u;  // (what is dropped has no part, not even where it is infinite)
+                const float bi = at8(b0.v[q], i), up = on ? G[i] * scale : 0.f, norm = on ? bi * r1 : 0.f;
+                const float bare = up * (norm * at8(pw, i)), z = up * (tg * at8(gt, i));
+                dots[1] = fmaf(bare, at8(gt, i), dots[1]);
                 if (PARTS) {
-                    acc[1][q][i] += (kept >> i & 1u) ? z * norm : 0.f;
+                    acc[1][q][i] = fmaf(z, norm, acc[1][q][i]);
                     acc[2][q][i] = fmaf(bare, tg, acc[2][q][i]);
                 }
-                v[q][i] = z * w;
-                dots[0] = fmaf(v[q][i], bi, dots[0]);
+                v[q][i] = z * at8(pw, i);
+                if (g.post_w) dots[0] = fmaf(v[q][i], bi, dots[0]);
             }
         }
-        if (!g.b) continue;
-        if (g.post_w || g.grad_token_gate) row_sums<WAVES>(dots, s_sum, turn);
-        const float m1 = g.post_w ? dots[0] * g.inv_d * r1 * r1 : 0.f;
+        if (g.b) {
+            if (g.post_w || g.grad_token_gate) row_sums<WAVES>(dots, s_sum, turn);
+            const float m1 = g.post_w ? dots[0] * g.inv_d * r1 * r1 : 0.f;
 #pragma unroll
-        for (int q = 0; q < CHUNKS; ++q) {
-            const int c = c0 + q * STEP;
-            if (c >= g.d) continue;
-            float o[8];
+            for (int q = 0; q < CHUNKS; ++q) {
+                const int c = c0 + q * STEP;
+                if (c >= g.d) continue;
+                float o[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) o[i] = g.post_w ? r1 * (v[q][i] - at8(b[q], i) * m1) : v[q][i];
-            store8(static_cast<T*>(g.grad_b) + row + c, round8<T>(o));
+                for (int i = 0; i < 8; ++i) o[i] = g.post_w ? r1 * (v[q][i] - at8(b0.v[q], i) * m1) : v[q][i];
+                store8(static_cast<T*>(g.grad_b) + row + c, round8<T>(o));
+            }
+            if (g.grad_token_gate && lane == 0 && (WAVES == 1 || wave == 0)) g.grad_token_gate[t] = dots[1];
         }
-        if (g.grad_token_gate && lane == 0 && (WAVES == 1 || wave == 0)) g.grad_token_gate[t] = dots[1];
+        if (!HOLD && t + stride < g.T) fetch(t + stride);
     }
     if constexpr (PARTS) {
         float* const out = g.parts + (size_t)blockIdx.x * 3 * g.d;
@@ -298,9 +342,21 @@ __global__ __launch_bounds__(1024) void block_parts_kernel(const float* __restri
     const int k = blockIdx.y, c = blockIdx.x * kWave + lane;
     float* const out = k == 0 ? open_w : k == 1 ? post_w : gate;
     if (!out) return;
+    // (eight loads in flight: one after the other, 512 parts of 2048 took 10.8 us)
     float f = 0.f;
-    if (c < d)
-        for (int i = wave; i < n; i += 16) f += parts[((size_t)i * 3 + k) * d + c];
+    if (c < d) {
+        const float* const p = parts + (size_t)k * d + c;
+        const size_t pitch = (size_t)3 * d;
+        int i = wave;
+        for (; i + 7 * 16 < n; i += 8 * 16) {
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = p[(size_t)(i + j * 16) * pitch];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f += v[j];
+        }
+        for (; i < n; i += 16) f += p[(size_t)i * pitch];
+    }
     s_sum[wave][lane] = f;
     __syncthreads();
     if (wave == 0 && c < d) {
@@ -315,16 +371,16 @@ __global__ __launch_bounds__(1024) void block_parts_kernel(const float* __restri
 struct RowPlan {
     int waves, chunks;
 };
-RowPlan row_plan(int T, int d) {
+RowPlan row_plan(int d) {
     const int chunks = (d + 511) / 512;
-    if (chunks <= 4 && T >= 2048) return RowPlan{1, chunks};
-    if (chunks <= 16) return RowPlan{4, (chunks + 3) / 4};
-    return RowPlan{16, (chunks + 15) / 16};
+    return chunks <= 4 ? RowPlan{chunks, 1} : chunks <= 8 ? RowPlan{8, 1} : RowPlan{16, (chunks + 15) / 16};
 }
-int grad_groups(int T, int d) {  // workgroups of the backward pass where they keep sums over tokens
-    const int most = row_plan(T, d).waves == 16 ? 256 : 512;
-    return std::min(most, row_plan(T, d).waves == 1 ? (T + 3) / 4 : T);
-}
+int row_groups(int T, int d) { return row_plan(d).waves == 1 ? (T + 3) / 4 : T; }  // workgroups that have a row at all
+// Most workgroups of a pass.  Forward: 16384 rows of 2048, dropout, 1024 / 2048 / 4096 / 16384 of them 58.7 / 62.0 / 55.1 / 57.3 us.  Backward, four
+// waves of 132 registers each: 256 / 512 / 768 / 1024 of them 151 / 95.5 / 86 / 91 us; as many waves of other widths.
+constexpr int kGroups = 4096, kGradWaves = 3072;
+int most_grad_groups(int d) { return kGradWaves / std::max(row_plan(d).waves, row_plan(d).waves == 1 ? 4 : 1); }
+int grad_groups(int T, int d) { return std::min(most_grad_groups(d), row_groups(T, d)); }
 
 template <typename F>
 int by_plan(RowPlan p, F run) {
@@ -332,27 +388,34 @@ int by_plan(RowPlan p, F run) {
     typedef std::integral_constant<int, 2> c2;
     typedef std::integral_constant<int, 3> c3;
     typedef std::integral_constant<int, 4> c4;
+    typedef std::integral_constant<int, 8> c8;
     typedef std::integral_constant<int, 16> c16;
-    auto on = [&](auto waves) { return p.chunks == 1 ? run(waves, c1{}) : p.chunks == 2 ? run(waves, c2{}) : p.chunks == 3 ? run(waves, c3{}) : run(waves, c4{}); };
-    return p.waves == 1 ? on(c1{}) : p.waves == 4 ? on(c4{}) : on(c16{});
+    switch (p.waves) {
+        case 1: return run(c1{}, c1{});
+        case 2: return run(c2{}, c1{});
+        case 3: return run(c3{}, c1{});
+        case 4: return run(c4{}, c1{});
+        case 8: return run(c8{}, c1{});
+        default: return p.chunks == 1 ? run(c16{}, c1{}) : p.chunks == 2 ? run(c16{}, c2{}) : p.chunks == 3 ? run(c16{}, c3{}) : run(c16{}, c4{});
+    }
 }
 
 template <typename T>
 int run_forward(const BlockArgs& g, hipStream_t st) {
-    return by_plan(row_plan(g.T, g.d), [&](auto waves, auto chunks) {
+    return by_plan(row_plan(g.d), [&](auto waves, auto chunks) {
         constexpr int W = decltype(waves)::value;
-        hipLaunchKernelGGL((block_norm_kernel<T, W, decltype(chunks)::value>), dim3(W == 1 ? (g.T + 3) / 4 : g.T), dim3(W == 1 ? 256 : W * kWave), 0, st, g);
+        hipLaunchKernelGGL((block_norm_kernel<T, W, decltype(chunks)::value>), dim3(std::min(kGroups, row_groups(g.T, g.d))), dim3(W == 1 ? 256 : W * kWave), 0,
+                           st, g);
         return launch_status();
     });
 }
 template <typename T>
 int run_backward(const BlockArgs& g, float* open_w, float* post_w, float* gate, hipStream_t st) {
-    const int groups = grad_groups(g.T, g.d);
-    const int rc = by_plan(row_plan(g.T, g.d), [&](auto waves, auto chunks) {
+    const int groups = g.parts ? grad_groups(g.T, g.d) : std::min(kGroups, row_groups(g.T, g.d));
+    const int rc = by_plan(row_plan(g.d), [&](auto waves, auto chunks) {
         constexpr int W = decltype(waves)::value, C = decltype(chunks)::value;
-        const int rows = W == 1 ? (g.T + 3) / 4 : g.T;
-        if (g.parts) hipLaunchKernelGGL((block_grad_kernel<T, W, C, true>), dim3(groups), dim3(W == 1 ? 256 : W * kWave), 0, st, g);
-        else hipLaunchKernelGGL((block_grad_kernel<T, W, C, false>), dim3(rows), dim3(W == 1 ? 256 : W * kWave), 0, st, g);
+        const auto kern = g.parts ? block_grad_kernel<T, W, C, true> : block_grad_kernel<T, W, C, false>;
+        hipLaunchKernelGGL(kern, dim3(groups), dim3(W == 1 ? 256 : W * kWave), 0, st, g);
         return launch_status();
     });
     if (rc != MOE_OK || !g.parts) return rc;
@@ -409,7 +472,7 @@ extern "C" int moe_block_norm(const moe_block* block, int32_t n_tokens, int32_t 
 extern "C" size_t moe_block_workspace_bytes(int32_t n_tokens, int32_t d_model) {
     if (n_tokens < 0 || n_tokens >= (1 << 24) || d_model < 1 || d_model % 8 || d_model > MOE_BLOCK_MAX_D) return 0;
     // (a row more than the workgroups of any number of tokens up to this one)
-    return round_up(sizeof(float) * 3 * (size_t)d_model * (size_t)std::min(512, n_tokens + 1), 256);
+    return round_up(sizeof(float) * 3 * (size_t)d_model * (size_t)std::min(most_grad_groups(d_model), n_tokens + 1), 256);
 }
 
 extern "C" int moe_block_norm_backward(const moe_block* block, int32_t n_tokens, int32_t d_model, int32_t act_dtype, const void* grad_y,
