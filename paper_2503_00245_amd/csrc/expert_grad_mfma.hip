@@ -14,8 +14,8 @@
 // Schedule: that of expert_gemm_pp.hip.  Eight waves in two groups half a k-step apart: one multiplies out of registers while the
 // other reads the fragments of its whole next step; fills go between the products, B by group 0, A by group 1.
 //
-// The activation's gradient needs a, b and dh of the same place: one workgroup forms all three for 96 columns (144
-// accumulator registers a lane, 80 for a step's fragments), a and b in a first pass over d, dh in a second one.  dh then is never rounded nor
+// The activation's gradient needs a, b and dh of the same place: one workgroup forms all three for 128 columns (192
+// accumulator registers a lane) or 96 (144), a and b in a first pass over d, dh in a second one.  dh then is never rounded nor
 // stored: as a tensor of its own in bf16 it raised the error of the gradients from 2.4e-3 to 2.9e-3.
 #include "expert_grad.h"
 #include "lds_fill.h"
@@ -35,6 +35,13 @@ constexpr int kSplitSlots = 32;  // one workgroup per CU
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
+// Gradients of weights are written past the caches: they are not read again here, and the weights and rows that are stay there (24 tokens of 1024 / 2816,
+// 4 of 16 experts: gx, whose weights the product before has read, 55 -> 31 us, a and b and dh 79 -> 70)
+__device__ __forceinline__ void store_past(void* p, uint4 v) {
+    typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+    __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), reinterpret_cast<u32x4*>(p));
+}
+
 // Four k-values of the lane's column, twice: rows at and at + rows4 of LDS
 __device__ __forceinline__ bf16x8 read_transposed(unsigned at, unsigned rows4) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -46,16 +53,16 @@ __device__ __forceinline__ bf16x8 read_transposed(unsigned at, unsigned rows4) {
 #endif
 }
 
-template <int OP>
+// COLS: output columns of a tile (ACT: 128 or 96; else 256)
+template <int OP, int COLS>
 struct Form {
     static constexpr bool ACT = OP == GRAD_ACT, WGT = OP == GRAD_WEIGHTS;
     static constexpr int WAVES_M = ACT ? 4 : 2, WAVES_N = 8 / WAVES_M;
     static constexpr int MB = 8 / WAVES_M;           // 32-row blocks of a wave: wm, wm + WAVES_M, ...
-    static constexpr int BN = ACT ? 128 : 256;       // output columns
-    static constexpr int NI = ACT ? 8 : 4;           // 16-column blocks of a wave (ACT: four of a, four of b, then four of dh)
-    static constexpr int SA = 2, SB = 3;             // k-steps in LDS
-    static constexpr int KS = ACT ? 2 : 1;           // phases that a k-step is multiplied in
-    static constexpr int A_BYTES = BM * BK * 2, B_BYTES = ACT ? 2 * BN * BK * 2 : BN * BK * 2;
+    static constexpr int NI = ACT ? COLS / 16 : 4;   // 16-column blocks of a wave (ACT: half of them a, half b; then half as many dh)
+    static constexpr int KS = COLS == 128 ? 2 : 1;   // phases that a k-step is multiplied in: with 192 accumulators a lane, half a step's fragments at a time
+    static constexpr int SA = 2, SB = COLS == 96 ? 4 : 3;  // k-steps in LDS
+    static constexpr int A_BYTES = BM * BK * 2, B_BYTES = (ACT ? 2 : 1) * COLS * BK * 2;
     static constexpr int LDS = SA * A_BYTES + SB * B_BYTES;
     static_assert(LDS <= 160 * 1024, "LDS of a CU");
 };
@@ -74,11 +81,11 @@ __device__ __forceinline__ int by_size(int count, int E) {
 }
 
 // PARTS (DX): the k-steps of a tile are cut into g.k_parts runs, each stored in fp32 to an output of its own
-template <int OP, bool PARTS>
+template <int OP, int COLS, bool PARTS>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void grad_kernel(const GradArgs g) {
-    typedef Form<OP> F;
+    typedef Form<OP, COLS> F;
     constexpr bool ACT = F::ACT, WGT = F::WGT;
-    constexpr int WAVES_M = F::WAVES_M, WAVES_N = F::WAVES_N, MB = F::MB, BN = F::BN, NI = F::NI, SA = F::SA, SB = F::SB, KS = F::KS;
+    constexpr int WAVES_M = F::WAVES_M, WAVES_N = F::WAVES_N, MB = F::MB, BN = COLS, NI = F::NI, SA = F::SA, SB = F::SB, KS = F::KS;
     constexpr int A_BYTES = F::A_BYTES, B_BYTES = F::B_BYTES, B_AT = SA * A_BYTES;
     extern __shared__ __align__(16) char smem[];
     const int lane = threadIdx.x & 63;
@@ -132,7 +139,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     // ---- fills.  Instruction p of wave w % 4 = fw writes the KB 4 p + fw of its operand's step; lane l the l-th 16 bytes of it.
     const unsigned lds0 = (unsigned)(uintptr_t)(lds_char*)smem;
     constexpr int PA = BM / 32;
-    constexpr int PB0 = 8, PB1 = ACT ? 4 : 8;  // of B in the first and in the second pass
+    constexpr int PB0 = F::B_BYTES / 4096, PB1 = ACT ? 4 : 8;  // of B in the first and in the second pass
     // rows of 128 bytes: row 8 (4 p + fw) + l / 8, slot l % 8 = chunk ^ (row / 2) % 8
     const int k_row = fw * 8 + (lane >> 3);
     const unsigned k_chunk = ((lane & 7) ^ (((fw & 1) << 2) | (lane >> 4))) * 16;
@@ -150,10 +157,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         for (int p = 0; p < 2; ++p) col[p] = (unsigned)min(m0 + (t_chunk ^ (p << 3)) * 8, M_pitch - 8) * 2;
     } else if (ACT) {
 #pragma unroll
-        for (int p = 0; p < 4; ++p) off[p] = (unsigned)min(n0 + k_row + 32 * p, N - 1) * ((unsigned)K * 2) + k_chunk;
-        // rows of 256 bytes: row 4 (4 p + fw) + l / 16
+        for (int p = 0; p < BN / 32; ++p) off[p] = (unsigned)min(n0 + k_row + 32 * p, N - 1) * ((unsigned)K * 2) + k_chunk;
+        // rows of 256 bytes (16 chunks; of 96 columns they are 12): row 4 (4 p + fw) + l / 16
         const int f = (lane >> 4) | (fw >> 1) << 2;
-        col[0] = (unsigned)min(n0 + ((lane & 15) ^ (f << 1)) * 8, N - 8) * 2 + (unsigned)(4 * fw + (lane >> 4)) * pitch_b;
+        col[0] = (unsigned)min(n0 + min((lane & 15) ^ (f << 1), BN / 8 - 1) * 8, N - 8) * 2 + (unsigned)(4 * fw + (lane >> 4)) * pitch_b;
     } else {
 #pragma unroll
         for (int p = 0; p < 2; ++p) col[p] = (unsigned)min(n0 + (t_chunk ^ (p << 3)) * 8, N - 8) * 2;
@@ -171,7 +178,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         if constexpr (GRP == 1 && !WGT) {
             dma16<false>(slot, (second ? A1 : A0) + k0 * 2, off[p]);
         } else if constexpr (GRP == 0 && ACT && S == 0) {
-            dma16<false>(slot, (p < 4 ? B0 : B1) + k0 * 2, off[p % 4]);
+            dma16<false>(slot, (p < PB0 / 2 ? B0 : B1) + k0 * 2, off[p % (PB0 / 2)]);
         } else if constexpr (GRP == 0 && ACT) {
             dma16<false>(slot, B2 + (size_t)(unsigned)(k0 + 16 * p) * pitch_b, col[0]);
         } else {
@@ -202,7 +209,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     // ---- fragment reads.  Rows of 128 bytes: row l % 16 of a block, chunk 4 ks + l / 16.
     const unsigned c16 = ((lane >> 4) ^ ((lane & 15) >> 1)) << 4;
     const unsigned ra = lds0 + wm * 4096 + (lane & 15) * 128 + c16;
-    const unsigned rb = lds0 + B_AT + wn * 64 * 128 + (lane & 15) * 128 + c16;  // (ACT, first pass)
+    const unsigned rb = lds0 + B_AT + wn * (BN / 2) * 128 + (lane & 15) * 128 + c16;  // (ACT, first pass)
     // rows read transposed: row 8 (l / 16) + (l % 16) / 4 (+ 4) of a 32-row half step, 8 bytes (l % 4) of unit u ^ f
     constexpr int T_ROW = ACT ? 256 : 512;
     const unsigned t_swz = (((lane & 15) >> 2) | ((lane >> 4) & 1) << 2) << 5;
@@ -229,9 +236,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                 for (int ni = 0; ni < N_I; ++ni) {
                     if constexpr (ACT && S == 0) {
                         fb[q][ni] = *reinterpret_cast<const __attribute__((address_space(3))) bf16x8*>(
-                            (uintptr_t)((rb ^ (ks << 6)) + pb + (ni / 4) * (128 * 128) + (ni % 4) * 2048));
+                            (uintptr_t)((rb ^ (ks << 6)) + pb + (ni / (NI / 2)) * (BN * 128) + (ni % (NI / 2)) * 2048));
                     } else if constexpr (ACT) {
-                        const unsigned unit = (unsigned)(wn * 4 + ni) << 5;
+                        const unsigned unit = (unsigned)(wn * (NI / 2) + ni) << 5;
                         fb[q][ni] = read_transposed((unit ^ swz) + (t_lane + B_AT + pb) + ks * (32 * T_ROW), 4 * T_ROW);
                     } else {
                         const unsigned unit = (unsigned)(wn * NI + ni) << 5;
@@ -391,7 +398,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
             const int r = it * RPI + rd_row;
             if ((64 % LPR || 32 % RPI) && (rd_row >= RPI || r >= 32)) continue;
             const uint4 v = *reinterpret_cast<const uint4*>(region + r * PITCH + rd_chunk * 16);
-            if (rbk + r < rows_here && n0 + c0 < N) *reinterpret_cast<uint4*>(out + (size_t)(rbk + r) * N + c0) = v;
+            if (rbk + r >= rows_here || n0 + c0 >= N) continue;
+            uint4* const to = reinterpret_cast<uint4*>(out + (size_t)(rbk + r) * N + c0);
+            if (WGT) store_past(to, v);
+            else *to = v;
         }
     };
     const size_t at0 = (size_t)m0 * N + n0;
@@ -438,12 +448,130 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     }
 }
 
-template <int OP, bool PARTS>
+// ---- gradients of weights from few rows -----------------------------------------------------------------------
+// A tile of few k-steps is mostly its beginning and its end: of 256 x 256 ones, alone on a CU, each took 10 us beside its steps.  Here two
+// workgroups share a CU, one's stores beside the other's products: tiles of 128 x 256 on four waves, k-steps of 32 rows, three of them in
+// LDS, one barrier a step.  A and B lie as in grad_kernel (A's rows of 256 bytes).
+constexpr int kWgtM = 128, kWgtN = 256, kWgtK = 32, kWgtStages = 3;
+// Rows of an expert, on average, below which (256 x 256 / these, us: 24 tokens of 1024 / 2816, 4 of 16 experts, 80 / 53, 777 of 1440 / 3840 117 / 99,
+// 2048 of 2048 / 5632 362 / 371, 16384 1675 / 1895)
+constexpr int kWgtSmallRows = 384;
+constexpr int kWgtA = kWgtM * kWgtK * 2, kWgtStage = (kWgtM + kWgtN) * kWgtK * 2, kWgtLds = kWgtStages * kWgtStage;
+
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void grad_weights_small_kernel(const GradArgs g) {
+    extern __shared__ __align__(16) char smem[];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave >> 1, wn = wave & 1;
+    int lo, hi;
+    group_bounds(g.offsets, g.E, g.P, lo, hi);
+    lo = min(max(lo, 0), g.P), hi = min(max(hi, lo), g.P);
+    // Strips of 256 hidden columns as in grad_kernel; for the gradients of W_gate and W_up a strip is two tiles high
+    const int dt = 2 * ((g.d + 255) / 256), ft = (g.F + 255) / 256, slot = blockIdx.x >> 3;
+    const int strip = uniform_div(slot, dt) * 8 + (blockIdx.x & 7), across = slot - uniform_div(slot, dt) * dt;
+    const int rank = uniform_div(strip, 3 * ft), in = strip - rank * 3 * ft;
+    if (rank >= g.E) return;
+    const int e = MOE_READLANE(by_size(hi - lo, g.E), rank);
+    const int which = uniform_div(in, ft), hidden = in - which * ft;
+    bf16_t* const out = static_cast<bf16_t*>(which == 0 ? g.gw_gate : which == 1 ? g.gw_up : g.gw_down);
+    const int M = which == 2 ? g.d : g.F, N = which == 2 ? g.F : g.d;
+    const int m0 = which == 2 ? across * kWgtM : hidden * 256 + (across & 1) * kWgtM, n0 = which == 2 ? hidden * kWgtN : (across >> 1) * kWgtN;
+    if (!out || m0 >= M || n0 >= N) return;
+    const int first = MOE_READLANE(lo, e), K = MOE_READLANE(hi, e) - first, nk = (K + kWgtK - 1) / kWgtK;
+    const unsigned pitch_a = (unsigned)M * 2, pitch_b = (unsigned)N * 2;
+    const char* const A = static_cast<const char*>(which == 0 ? g.da : which == 1 ? g.db : g.gy) + (size_t)first * pitch_a;
+    const char* const B = static_cast<const char*>(which == 2 ? g.h : g.x) + (size_t)first * pitch_b;
+
+    // fills of a step: A by KB 4 p + wave, p < 2 (row 4 (4 p + wave) + l / 16), B by KB 4 p + wave, p < 4 (row 2 (4 p + wave) + l / 32)
+    const unsigned lds0 = (unsigned)(uintptr_t)(lds_char*)smem;
+    const int a_row = 4 * wave + (lane >> 4), b_row = 2 * wave + (lane >> 5);
+    const int a_f = (lane >> 4) | (wave >> 1) << 2;
+    const unsigned a_col = (unsigned)min(m0 + ((lane & 15) ^ (a_f << 1)) * 8, M - 8) * 2;
+    const int b_chunk = (lane & 31) ^ ((b_row & 3) << 1);
+    unsigned b_col[2];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) b_col[p] = (unsigned)min(n0 + (b_chunk ^ (p << 3)) * 8, N - 8) * 2;
+    auto fill = [&](int v, auto last) INLINE {
+        const int k0 = v * kWgtK, left = K - 1 - k0;  // (the last step: rows past the end are the last one again)
+        const unsigned at = lds0 + v % kWgtStages * kWgtStage + wave * 1024;
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const int r = decltype(last)::value ? min(a_row + 16 * p, left) : a_row + 16 * p;
+            dma16<false>(at + p * 4096, A + (size_t)(unsigned)k0 * pitch_a, (unsigned)r * pitch_a + a_col);
+        }
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+            const int r = decltype(last)::value ? min(b_row + 8 * p, left) : b_row + 8 * p;
+            dma16<false>(at + kWgtA + p * 4096, B + (size_t)(unsigned)k0 * pitch_b, (unsigned)r * pitch_b + b_col[p & 1]);
+        }
+    };
+    auto fill_any = [&](int v) INLINE {
+        if (v == nk - 1) fill(v, std::true_type{});
+        else fill(v, std::false_type{});
+    };
+    f32x4 acc[4][8];
+#pragma unroll
+    for (int mi = 0; mi < 4; ++mi)
+#pragma unroll
+        for (int ni = 0; ni < 8; ++ni) acc[mi][ni] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const unsigned t_row = 8 * (lane >> 4) + ((lane & 15) >> 2), t_byte = (lane & 3) * 8;
+    const unsigned swz = (((lane & 15) >> 2) | ((lane >> 4) & 1) << 2) << 5;
+    if (nk > 0) fill_any(0);
+    if (nk > 1) fill_any(1);
+    for (int v = 0; v < nk; ++v) {
+        if (v + 1 < nk) wait_vm<6>();  // step v has landed
+        else wait_vm<0>();
+        phase_end();                   // and that before it has been read
+        if (v + 2 < nk) fill_any(v + 2);
+        const unsigned pa = lds0 + v % kWgtStages * kWgtStage + t_row * 256 + t_byte, pb = lds0 + v % kWgtStages * kWgtStage + kWgtA + t_row * 512 + t_byte;
+        bf16x8 fa[4], fb[8];
+#pragma unroll
+        for (int mi = 0; mi < 4; ++mi) fa[mi] = read_transposed(pa + (((unsigned)(wm * 4 + mi) << 5) ^ swz), 4 * 256);
+#pragma unroll
+        for (int ni = 0; ni < 8; ++ni) fb[ni] = read_transposed(pb + (((unsigned)(wn * 8 + ni) << 5) ^ swz), 4 * 512);
+        if (v == nk - 1 && K % kWgtK) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const bool past = (lane >> 4) * 8 + j >= K - v * kWgtK;
+#pragma unroll
+                for (int mi = 0; mi < 4; ++mi) fa[mi][j] = past ? (bf16_t)0.f : fa[mi][j];
+            }
+        }
+#pragma unroll
+        for (int ni = 0; ni < 8; ++ni)
+#pragma unroll
+            for (int mi = 0; mi < 4; ++mi) acc[mi][ni] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[ni], fa[mi], acc[mi][ni], 0, 0, 0);
+    }
+    phase_end();
+    // 16 rows at a time through LDS, a region per wave, so that the tile leaves in 16-byte stores: row l % 16, columns 4 (l / 16) .. + 4 of a block
+    constexpr int PITCH = 128 * 2 + 16;
+    char* const region = smem + wave * (16 * PITCH);
+    bf16_t* const to = out + (size_t)e * g.d * g.F + (size_t)m0 * N + n0;
+#pragma unroll
+    for (int mi = 0; mi < 4; ++mi) {
+#pragma unroll
+        for (int ni = 0; ni < 8; ++ni) {
+            bf16x4 o;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[j] = (bf16_t)acc[mi][ni][j];
+            *reinterpret_cast<bf16x4*>(region + (lane & 15) * PITCH + ni * 32 + (lane >> 4) * 8) = o;
+        }
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+            const int r = it * 4 + (lane >> 4), row = wm * 64 + mi * 16 + r, c = wn * 128 + (lane & 15) * 8;
+            const uint4 v = *reinterpret_cast<const uint4*>(region + r * PITCH + (lane & 15) * 16);
+            if (m0 + row < M && n0 + c < N) store_past(to + (size_t)row * N + c, v);
+        }
+    }
+}
+
+template <int OP, int COLS, bool PARTS>
 int launch(const GradArgs& g, int grid, hipStream_t st) {
     static std::atomic<uint64_t> lds_allowed;
-    const auto kern = grad_kernel<OP, PARTS>;
-    if (allow_dynamic_lds(reinterpret_cast<const void*>(kern), Form<OP>::LDS, lds_allowed) != MOE_OK) return MOE_ERR_LAUNCH;
-    hipLaunchKernelGGL(kern, dim3(grid), dim3(kThreads), Form<OP>::LDS, st, g);
+    constexpr int lds = Form<OP, COLS>::LDS;
+    const auto kern = grad_kernel<OP, COLS, PARTS>;
+    if (allow_dynamic_lds(reinterpret_cast<const void*>(kern), lds, lds_allowed) != MOE_OK) return MOE_ERR_LAUNCH;
+    hipLaunchKernelGGL(kern, dim3(grid), dim3(kThreads), lds, st, g);
     return launch_status();
 }
 
@@ -455,6 +583,12 @@ bool grad_mfma_supported(const GradArgs& g) {
     return d > 2 * BK && F > 2 * BK && P * d * 2 < (1ll << 32) && P * F * 2 < (1ll << 32) && d * F * 2 < (1ll << 32);
 }
 
+// Row tiles that a layer's groups are expected to need: beside whole ones about half a tile each, a little more as loads are uneven
+static double tiles_expected(const GradArgs& g) {
+    const double groups = std::min(g.P, g.E);
+    return std::max(groups, g.P / 256.0 + 0.6 * groups);
+}
+
 // ---- gx in parts --------------------------------------------------------------------------------------
 // Its tiles are few (rows by d, where the other products have F or F by d) and long (2 F deep).  Where they do not fill the CUs their k-steps are cut
 // into up to four runs, summed by a launch of its own in fp32.  A model of the launch in us decides: rounds of 256 workgroups (the last
@@ -463,7 +597,7 @@ size_t grad_parts_bytes(long long P, int d) {  // room for them; does not fall a
     return std::min<size_t>(16 * (size_t)P * d, 200u << 20);
 }
 int grad_parts(const GradArgs& g) {
-    const double groups = std::min(g.P, g.E), m = std::max(groups, g.P / 256.0 + 0.6 * groups), tiles = m * ((g.d + 255) / 256);
+    const double groups = std::min(g.P, g.E), tiles = tiles_expected(g) * ((g.d + 255) / 256);
     const double step = std::max(0.8, 1.15 * std::min(1.0, g.P / groups / 192)), steps = 2 * ((g.F + BK - 1) / BK);
     const int most = (int)std::min<size_t>(4, grad_parts_bytes(g.P, g.d) / (4 * (size_t)g.P * g.d));
     int best = 1;
@@ -497,15 +631,27 @@ __global__ __launch_bounds__(256) void sum_grad_parts_kernel(const float* __rest
 int run_grad_mfma(const GradArgs& g, GradOp op, hipStream_t st) {
     if (op == GRAD_WEIGHTS) {
         const int strips = g.E * 3 * ((g.F + 255) / 256);
-        return launch<GRAD_WEIGHTS, false>(g, (strips + 7) / 8 * 8 * ((g.d + 255) / 256), st);
+        if (g.P < (long long)kWgtSmallRows * g.E) {
+            static std::atomic<uint64_t> lds_allowed;
+            if (allow_dynamic_lds(reinterpret_cast<const void*>(grad_weights_small_kernel), kWgtLds, lds_allowed) != MOE_OK) return MOE_ERR_LAUNCH;
+            hipLaunchKernelGGL(grad_weights_small_kernel, dim3((strips + 7) / 8 * 8 * 2 * ((g.d + 255) / 256)), dim3(256), kWgtLds, st, g);
+            return launch_status();
+        }
+        return launch<GRAD_WEIGHTS, 256, false>(g, (strips + 7) / 8 * 8 * ((g.d + 255) / 256), st);
     }
     const int m = m_tiles_bound(g.P, g.E, BM);
-    if (op == GRAD_ACT) return launch<GRAD_ACT, false>(g, find_tile_grid(m * ((g.F + Form<GRAD_ACT>::BN - 1) / Form<GRAD_ACT>::BN), kSplitSlots), st);
+    if (op == GRAD_ACT) {
+        // Tiles of 128 columns take 1.21 times as long as tiles of 96; whole rounds decide (us, 96 / 128: 24 tokens of 1024 / 2816, 4 of 16
+        // experts, 67.5 / 79, 777 of 1440 / 3840 133 / 140, 2048 of 2048 / 5632 353 / 346, 16384 2365 / 2140)
+        auto rounds = [&](int cols) { return std::ceil(tiles_expected(g) * ((g.F + cols - 1) / cols) / 256); };
+        if (1.21 * rounds(128) < rounds(96)) return launch<GRAD_ACT, 128, false>(g, find_tile_grid(m * ((g.F + 127) / 128), kSplitSlots), st);
+        return launch<GRAD_ACT, 96, false>(g, find_tile_grid(m * ((g.F + 95) / 96), kSplitSlots), st);
+    }
     const int tiles = m * ((g.d + 255) / 256), parts = grad_parts(g);
-    if (parts == 1) return launch<GRAD_DX, false>(g, find_tile_grid(tiles, kSplitSlots), st);
+    if (parts == 1) return launch<GRAD_DX, 256, false>(g, find_tile_grid(tiles, kSplitSlots), st);
     GradArgs cut = g;
     cut.k_parts = parts;
-    const int rc = launch<GRAD_DX, true>(cut, find_tile_grid(tiles * parts, kSplitSlots), st);
+    const int rc = launch<GRAD_DX, 256, true>(cut, find_tile_grid(tiles * parts, kSplitSlots), st);
     if (rc != MOE_OK) return rc;
     const long long chunks = (long long)g.P * g.d / 8;
     hipLaunchKernelGGL(sum_grad_parts_kernel, dim3((unsigned)std::min<long long>((chunks + 255) / 256, 2048)), dim3(256), 0, st, g.parts, parts, g.offsets, g.E,
