@@ -29,7 +29,7 @@ namespace {
 
 #define INLINE __attribute__((always_inline))
 
-constexpr int BM = 256, BK = 64, kThreads = 512;
+constexpr int BK = 64, kThreads = 512;
 constexpr int kSplitSlots = 32;  // one workgroup per CU
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -53,15 +53,15 @@ __device__ __forceinline__ bf16x8 read_transposed(unsigned at, unsigned rows4) {
 #endif
 }
 
-// COLS: output columns of a tile (ACT: 128 or 96; else 256)
-template <int OP, int COLS>
+// BM, COLS: rows and output columns of a tile (DX, WEIGHTS: 256 columns)
+template <int OP, int BM, int COLS>
 struct Form {
     static constexpr bool ACT = OP == GRAD_ACT, WGT = OP == GRAD_WEIGHTS;
-    static constexpr int WAVES_M = ACT ? 4 : 2, WAVES_N = 8 / WAVES_M;
-    static constexpr int MB = 8 / WAVES_M;           // 32-row blocks of a wave: wm, wm + WAVES_M, ...
-    static constexpr int NI = ACT ? COLS / 16 : 4;   // 16-column blocks of a wave (ACT: half of them a, half b; then half as many dh)
-    static constexpr int KS = COLS == 128 ? 2 : 1;   // phases that a k-step is multiplied in: with 192 accumulators a lane, half a step's fragments at a time
-    static constexpr int SA = 2, SB = COLS == 96 ? 4 : 3;  // k-steps in LDS
+    static constexpr int WAVES_M = ACT && BM == 256 ? 4 : 2, WAVES_N = 8 / WAVES_M;
+    static constexpr int MB = BM / 32 / WAVES_M;     // 32-row blocks of a wave: wm, wm + WAVES_M, ...
+    static constexpr int NI = (ACT ? 2 : 1) * COLS / WAVES_N / 16;  // 16-column blocks of a wave (ACT: half of them a, half b; then half as many dh)
+    static constexpr int KS = ACT && BM == 256 && COLS == 128 ? 2 : 1;  // phases that a k-step is multiplied in: with 192 accumulators a lane, half a step's fragments at a time
+    static constexpr int SA = BM == 128 ? 4 : 2, SB = COLS == 96 ? 4 : 3;  // k-steps in LDS
     static constexpr int A_BYTES = BM * BK * 2, B_BYTES = (ACT ? 2 : 1) * COLS * BK * 2;
     static constexpr int LDS = SA * A_BYTES + SB * B_BYTES;
     static_assert(LDS <= 160 * 1024, "LDS of a CU");
@@ -81,9 +81,9 @@ __device__ __forceinline__ int by_size(int count, int E) {
 }
 
 // PARTS (DX): the k-steps of a tile are cut into g.k_parts runs, each stored in fp32 to an output of its own
-template <int OP, int COLS, bool PARTS>
+template <int OP, int BM, int COLS, bool PARTS>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void grad_kernel(const GradArgs g) {
-    typedef Form<OP, COLS> F;
+    typedef Form<OP, BM, COLS> F;
     constexpr bool ACT = F::ACT, WGT = F::WGT;
     constexpr int WAVES_M = F::WAVES_M, WAVES_N = F::WAVES_N, MB = F::MB, BN = COLS, NI = F::NI, SA = F::SA, SB = F::SB, KS = F::KS;
     constexpr int A_BYTES = F::A_BYTES, B_BYTES = F::B_BYTES, B_AT = SA * A_BYTES;
@@ -209,7 +209,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     // ---- fragment reads.  Rows of 128 bytes: row l % 16 of a block, chunk 4 ks + l / 16.
     const unsigned c16 = ((lane >> 4) ^ ((lane & 15) >> 1)) << 4;
     const unsigned ra = lds0 + wm * 4096 + (lane & 15) * 128 + c16;
-    const unsigned rb = lds0 + B_AT + wn * (BN / 2) * 128 + (lane & 15) * 128 + c16;  // (ACT, first pass)
+    const unsigned rb = lds0 + B_AT + wn * (BN / WAVES_N) * 128 + (lane & 15) * 128 + c16;  // (ACT, first pass)
     // rows read transposed: row 8 (l / 16) + (l % 16) / 4 (+ 4) of a 32-row half step, 8 bytes (l % 4) of unit u ^ f
     constexpr int T_ROW = ACT ? 256 : 512;
     const unsigned t_swz = (((lane & 15) >> 2) | ((lane >> 4) & 1) << 2) << 5;
@@ -565,11 +565,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     }
 }
 
-template <int OP, int COLS, bool PARTS>
+template <int OP, int BM, int COLS, bool PARTS>
 int launch(const GradArgs& g, int grid, hipStream_t st) {
     static std::atomic<uint64_t> lds_allowed;
-    constexpr int lds = Form<OP, COLS>::LDS;
-    const auto kern = grad_kernel<OP, COLS, PARTS>;
+    constexpr int lds = Form<OP, BM, COLS>::LDS;
+    const auto kern = grad_kernel<OP, BM, COLS, PARTS>;
     if (allow_dynamic_lds(reinterpret_cast<const void*>(kern), lds, lds_allowed) != MOE_OK) return MOE_ERR_LAUNCH;
     hipLaunchKernelGGL(kern, dim3(grid), dim3(kThreads), lds, st, g);
     return launch_status();
@@ -584,9 +584,9 @@ bool grad_mfma_supported(const GradArgs& g) {
 }
 
 // Row tiles that a layer's groups are expected to need: beside whole ones about half a tile each, a little more as loads are uneven
-static double tiles_expected(const GradArgs& g) {
+static double tiles_expected(const GradArgs& g, int bm) {
     const double groups = std::min(g.P, g.E);
-    return std::max(groups, g.P / 256.0 + 0.6 * groups);
+    return std::max(groups, (double)g.P / bm + 0.6 * groups);
 }
 
 // ---- gx in parts --------------------------------------------------------------------------------------
@@ -597,7 +597,7 @@ size_t grad_parts_bytes(long long P, int d) {  // room for them; does not fall a
     return std::min<size_t>(16 * (size_t)P * d, 200u << 20);
 }
 int grad_parts(const GradArgs& g) {
-    const double groups = std::min(g.P, g.E), tiles = tiles_expected(g) * ((g.d + 255) / 256);
+    const double groups = std::min(g.P, g.E), tiles = tiles_expected(g, 256) * ((g.d + 255) / 256);
     const double step = std::max(0.8, 1.15 * std::min(1.0, g.P / groups / 192)), steps = 2 * ((g.F + BK - 1) / BK);
     const int most = (int)std::min<size_t>(4, grad_parts_bytes(g.P, g.d) / (4 * (size_t)g.P * g.d));
     int best = 1;
@@ -637,21 +637,24 @@ int run_grad_mfma(const GradArgs& g, GradOp op, hipStream_t st) {
             hipLaunchKernelGGL(grad_weights_small_kernel, dim3((strips + 7) / 8 * 8 * 2 * ((g.d + 255) / 256)), dim3(256), kWgtLds, st, g);
             return launch_status();
         }
-        return launch<GRAD_WEIGHTS, 256, false>(g, (strips + 7) / 8 * 8 * ((g.d + 255) / 256), st);
+        return launch<GRAD_WEIGHTS, 256, 256, false>(g, (strips + 7) / 8 * 8 * ((g.d + 255) / 256), st);
     }
-    const int m = m_tiles_bound(g.P, g.E, BM);
     if (op == GRAD_ACT) {
-        // Tiles of 128 columns take 1.21 times as long as tiles of 96; whole rounds decide (us, 96 / 128: 24 tokens of 1024 / 2816, 4 of 16
-        // experts, 67.5 / 79, 777 of 1440 / 3840 133 / 140, 2048 of 2048 / 5632 353 / 346, 16384 2365 / 2140)
-        auto rounds = [&](int cols) { return std::ceil(tiles_expected(g) * ((g.F + cols - 1) / cols) / 256); };
-        if (1.21 * rounds(128) < rounds(96)) return launch<GRAD_ACT, 128, false>(g, find_tile_grid(m * ((g.F + 127) / 128), kSplitSlots), st);
-        return launch<GRAD_ACT, 96, false>(g, find_tile_grid(m * ((g.F + 95) / 96), kSplitSlots), st);
+        // 256 rows by 128 columns take 1.21 times as long as by 96, 128 rows by 128 0.72 times; whole rounds decide, and near empty
+        // tiles are bound by the weights (us, 256 x 96 / 256 x 128 / 128 x 128: 24 tokens of 1024 / 2816, 4 of 16 experts, 57 / 70 / 59, 777 of 1440 / 3840
+        // 133 / 140 / 114, 2048 of 2048 / 5632 353 / 346 / 363, 16384 2365 / 2140 / 2380)
+        auto tiles = [&](int bm, int cols) { return m_tiles_bound(g.P, g.E, bm) * ((g.F + cols - 1) / cols); };
+        auto cost = [&](int bm, int cols, double tile) { return tile * std::ceil(tiles_expected(g, bm) * ((g.F + cols - 1) / cols) / 256); };
+        const double wide = cost(256, 128, 1.21), narrow = cost(256, 96, 1.0), low = cost(128, 128, 0.72);
+        if (low < wide && low < narrow && g.P > 32ll * g.E && g.d > 3 * BK) return launch<GRAD_ACT, 128, 128, false>(g, find_tile_grid(tiles(128, 128), kSplitSlots), st);
+        if (wide < narrow) return launch<GRAD_ACT, 256, 128, false>(g, find_tile_grid(tiles(256, 128), kSplitSlots), st);
+        return launch<GRAD_ACT, 256, 96, false>(g, find_tile_grid(tiles(256, 96), kSplitSlots), st);
     }
-    const int tiles = m * ((g.d + 255) / 256), parts = grad_parts(g);
-    if (parts == 1) return launch<GRAD_DX, 256, false>(g, find_tile_grid(tiles, kSplitSlots), st);
+    const int tiles = m_tiles_bound(g.P, g.E, 256) * ((g.d + 255) / 256), parts = grad_parts(g);
+    if (parts == 1) return launch<GRAD_DX, 256, 256, false>(g, find_tile_grid(tiles, kSplitSlots), st);
     GradArgs cut = g;
     cut.k_parts = parts;
-    const int rc = launch<GRAD_DX, 256, true>(cut, find_tile_grid(tiles * parts, kSplitSlots), st);
+    const int rc = launch<GRAD_DX, 256, 256, true>(cut, find_tile_grid(tiles * parts, kSplitSlots), st);
     if (rc != MOE_OK) return rc;
     const long long chunks = (long long)g.P * g.d / 8;
     hipLaunchKernelGGL(sum_grad_parts_kernel, dim3((unsigned)std::min<long long>((chunks + 255) / 256, 2048)), dim3(256), 0, st, g.parts, parts, g.offsets, g.E,
