@@ -511,8 +511,10 @@ def _workspace(workspace: Optional[torch.Tensor], device: int):
 
 
 def _stream_on(device: int) -> int:
-    """_stream of a device's index (-1: host tensors, which no launch is reached with)"""
-    return _raw_stream(device) if _raw_stream is not None and device >= 0 else torch.cuda.current_stream().cuda_stream if device >= 0 else 0
+    """_stream of a device's index; host tensors, which have none, are refused: the library takes pointers and cannot tell"""
+    if device < 0:
+        raise ValueError("tensors must be on a GPU")
+    return torch.cuda.current_stream(device).cuda_stream if _raw_stream is None else _raw_stream(device)
 
 
 def _layer_sizes(shape: MoeShape):

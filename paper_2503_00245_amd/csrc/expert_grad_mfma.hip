@@ -126,8 +126,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
             nt -= part * n_tiles;
         }
         n0 = nt * BN;
-        A0 = static_cast<const char*>(ACT ? g.x : g.da), A1 = static_cast<const char*>(ACT ? g.gy : g.db);
-        B0 = static_cast<const char*>(g.w_gate) + e * at_w, B1 = static_cast<const char*>(g.w_up) + e * at_w;
+        const size_t at_row = (size_t)m0 * M_pitch * 2, at_col = ACT ? (size_t)n0 * K * 2 : 0;  // (rows of 128 bytes: from the tile's first on)
+        A0 = static_cast<const char*>(ACT ? g.x : g.da) + at_row, A1 = static_cast<const char*>(ACT ? g.gy : g.db) + at_row;
+        B0 = static_cast<const char*>(g.w_gate) + e * at_w + at_col, B1 = static_cast<const char*>(g.w_up) + e * at_w + at_col;
         if (ACT) B2 = static_cast<const char*>(g.w_down) + e * at_w;
     }
     const int nk = (K + BK - 1) / BK;              // k-steps of a pass
@@ -151,13 +152,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     unsigned off[8], col[2] = {};
     if (grp == 1 && !WGT) {
 #pragma unroll
-        for (int p = 0; p < PA; ++p) off[p] = (unsigned)min(m0 + k_row + 32 * p, m_end - 1) * pitch_a + k_chunk;
+        for (int p = 0; p < PA; ++p) off[p] = (unsigned)min(k_row + 32 * p, m_end - 1 - m0) * pitch_a + k_chunk;
     } else if (grp == 1) {
 #pragma unroll
         for (int p = 0; p < 2; ++p) col[p] = (unsigned)min(m0 + (t_chunk ^ (p << 3)) * 8, M_pitch - 8) * 2;
     } else if (ACT) {
 #pragma unroll
-        for (int p = 0; p < BN / 32; ++p) off[p] = (unsigned)min(n0 + k_row + 32 * p, N - 1) * ((unsigned)K * 2) + k_chunk;
+        for (int p = 0; p < BN / 32; ++p) off[p] = (unsigned)min(k_row + 32 * p, N - 1 - n0) * ((unsigned)K * 2) + k_chunk;
         // rows of 256 bytes (16 chunks; of 96 columns they are 12): row 4 (4 p + fw) + l / 16
         const int f = (lane >> 4) | (fw >> 1) << 2;
         col[0] = (unsigned)min(n0 + min((lane & 15) ^ (f << 1), BN / 8 - 1) * 8, N - 8) * 2 + (unsigned)(4 * fw + (lane >> 4)) * pitch_b;
@@ -577,11 +578,8 @@ int launch(const GradArgs& g, int grid, hipStream_t st) {
 
 }  // namespace
 
-// Offsets within an operand's rows are 32 bits, and a pass has as many k-steps as are fetched ahead of the first
-bool grad_mfma_supported(const GradArgs& g) {
-    const long long d = g.d, F = g.F, P = g.P;
-    return d > 2 * BK && F > 2 * BK && P * d * 2 < (1ll << 32) && P * F * 2 < (1ll << 32) && d * F * 2 < (1ll << 32);
-}
+// A pass has as many k-steps as are fetched ahead of the first.  (Offsets within a tile, of 256 rows of at most 2^18 values, are 32 bits.)
+bool grad_mfma_supported(const GradArgs& g) { return g.d > 2 * BK && g.F > 2 * BK; }
 
 // Row tiles that a layer's groups are expected to need: beside whole ones about half a tile each, a little more as loads are uneven
 static double tiles_expected(const GradArgs& g, int bm) {

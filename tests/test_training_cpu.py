@@ -228,6 +228,24 @@ def test_binding_refuses():
         pkg.moe_block_stack_forward(shape, [pkg.MoeWeights()], [], [], t(3, 16), t(3, 16))
 
 
+def test_binding_refuses_host_tensors():
+    # they have the right types and shapes, and nothing but the device tells them from what the library takes
+    shape = pkg.make_shape(3, 16, 8, 4, 2, act_dtype=pkg.MOE_F32)
+    x, rows, gate = torch.zeros(3, 16), torch.zeros(6, 16), torch.zeros(3, 2)
+    idx, inv, off = (torch.zeros(*s, dtype=torch.int32) for s in ((3, 2), (6,), (5,)))
+    w = torch.zeros(4, 8, 16)
+    calls = [lambda: pkg.moe_dispatch(shape, idx, None, x, off, inv, inv.clone(), rows, torch.zeros(1 << 16)),
+             lambda: pkg.moe_dispatch_backward(shape, rows, inv, None, gate, x), lambda: pkg.moe_collect(shape, rows, inv, gate, None, x),
+             lambda: pkg.moe_collect_backward(shape, x, rows, off, inv, gate, rows.clone(), gate.clone()),
+             lambda: pkg.moe_expert_ffn_backward(shape, pkg.MoeWeights(), rows, off, rows, rows.clone(), w, workspace=torch.zeros(1 << 16)),
+             lambda: pkg.moe_block_norm(pkg.make_block(), x, x, None, x.clone(), None),
+             lambda: pkg.moe_block_norm_backward(pkg.make_block(), x, None, None, x, None, x.clone(), x.clone()),
+             lambda: pkg.moe_block_stack_forward(shape, [pkg.MoeWeights()], [pkg.make_block()], [torch.zeros(16)], x, x.clone())]
+    for call_ in calls:
+        with pytest.raises(ValueError, match="GPU"):
+            call_()
+
+
 # ---- the plain implementations themselves ---------------------------------------------------------------------------
 
 def _f64(g, *shape):

@@ -175,6 +175,49 @@ def test_gradient_of_the_experts(T, d, F, E, k, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,d,F,E,k", [(1, 128, 256, 8, 2), (8, 256, 512, 4, 2), (40, 432, 1152, 8, 2), (300, 1024, 264, 4, 2), (2000, 136, 520, 8, 2)])
+def test_experts_of_a_batch_with_padding(T, d, F, E, k, dtype):
+    # the forward pass on what moe_dispatch leaves: rows behind the last group are neither read nor written
+    dt = DTYPES[dtype]
+    for masked in (0.4, 1.0):
+        shape, _, offsets, x, _, w = _experts(T, d, F, E, k, dt, masked)
+        wd = [t.to(dev()) for t in w]
+        y = torch.full((T * k, d), -7.0, dtype=dt, device=dev())
+        weights = pkg.make_weights(dict(zip(("w_gate", "w_up", "w_down"), wd)))
+        pkg.moe_expert_ffn(shape, weights, x.to(dev()), torch.tensor(offsets, dtype=torch.int32, device=dev()), y, pkg.alloc_workspace(shape, dev()))
+        live = offsets[-1]
+        to.near(y[:live], to.experts_forward(x.to(dev()), offsets, *wd, dt), "y_perm")
+        assert (y[live:] == -7.0).all()
+
+
+def test_gradient_of_the_experts_beyond_32_bit_offsets():
+    # 2^21 pairs of 1032 hidden values are over 4 GB a tensor; one row in 4096 is compared
+    T, d, F, E = 1 << 21, 136, 1032, 2
+    g = torch.Generator(device=dev())
+    g.manual_seed(3)
+    shape, ws = make(T, d, E, 1, torch.bfloat16, F)
+    x, gy = (torch.randn(T, d, generator=g, device=dev()).bfloat16() for _ in range(2))
+    w = [(torch.randn(E, *s, generator=g, device=dev()) * s[1] ** -0.5).bfloat16() for s in ((F, d), (F, d), (d, F))]
+    offsets = [0, 3 * T // 4, T]
+    gx = torch.full_like(x, float("nan"))
+    weights = pkg.make_weights(dict(zip(("w_gate", "w_up", "w_down"), w)))
+    pkg.moe_expert_ffn_backward(shape, weights, x, torch.tensor(offsets, dtype=torch.int32, device=dev()), gy, gx, workspace=ws)
+    pick = torch.cat([torch.arange(0, T, 4096, device=dev()), torch.tensor([offsets[1] - 1, offsets[1], T - 1], device=dev())]).sort().values
+    n0 = int((pick < offsets[1]).sum())
+    want = to.experts_grad(x[pick], [0, n0, len(pick)], gy[pick], *w, torch.bfloat16)[0]
+    to.near(gx[pick], want, "grad_x_perm")
+    # gradients of weights: every row the same, so that they are one row's times their number, exactly in powers of two
+    del gx
+    x[:], gy[:] = 0, 0
+    x[:, 0], gy[:, 0] = 1, 1
+    out = [torch.empty_like(t) for t in w]
+    pkg.moe_expert_ffn_backward(shape, weights, x, torch.tensor([0, T, T], dtype=torch.int32, device=dev()), gy, None, *out, ws)
+    one = to.experts_grad(x[:1], [0, 1, 1], gy[:1], *w, torch.bfloat16)[1:]
+    for o, (v, b) in zip(out, one):  # (a sum of T equal terms in fp32 is T terms' roundings)
+        to.near(o, (v * T, (b + v.abs() * T * to.U32 + to.HALF[torch.bfloat16] * v.abs()) * T))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_gradient_of_the_experts_of_no_tokens(dtype):
     shape, ws, _, x, gy, w = _experts(0, 64, 136, 4, 2, DTYPES[dtype], seed=5)
     outs = _backward(shape, ws, torch.zeros(5, dtype=torch.int32, device=dev()), x.to(dev()), gy.to(dev()), [t.to(dev()) for t in w])

@@ -111,6 +111,26 @@ def experts_grad(x, offsets, gy, wg, wu, wd, dtype):
     return list(zip(outs, bounds))
 
 
+def experts_forward(x, offsets, wg, wu, wd, dtype):
+    """y_perm of the rows that have a group, with its bound: h and y are rounded, and a product's k-steps may be summed in two to four parts of
+    the storage type"""
+    u, live, d, F = HALF[dtype], offsets[-1], x.shape[1], wg.shape[1]
+    v, bound = torch.zeros(live, d, dtype=torch.float64, device=x.device), torch.zeros(live, d, dtype=torch.float64, device=x.device)
+    for e in range(wg.shape[0]):
+        lo, hi = offsets[e], offsets[e + 1]
+        X, Wg, Wu, Wd = (t.double() for t in (x[lo:hi], wg[e], wu[e], wd[e]))
+        a, b = X @ Wg.T, X @ Wu.T
+        ea, eb = (d + 2) * U32 * (X.abs() @ Wg.abs().T), (d + 2) * U32 * (X.abs() @ Wu.abs().T)
+        act = a * torch.sigmoid(a)
+        h = act * b
+        eh = act.abs() * eb + b.abs() * (1.1 * ea + act.abs() * (1.5 * a.abs() + 8) * U32) + 4 * U32 * h.abs()
+        eh = eh + u * (h.abs() + eh)
+        size = (h.abs() + eh) @ Wd.abs().T
+        v[lo:hi] = h @ Wd.T
+        bound[lo:hi] = eh @ Wd.abs().T + (F + 2) * U32 * size + 2 * u * size
+    return v, bound
+
+
 # ---- block ------------------------------------------------------------------------------------------------------
 
 def philox(counter, key):
