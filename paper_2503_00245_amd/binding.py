@@ -501,7 +501,7 @@ def alloc_training_workspace(shape: MoeShape, device) -> torch.Tensor:
 
 
 def _bytes(workspace: Optional[torch.Tensor]) -> int:
-    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return 0 if workspace is None else workspace.nbytes
 
 
 def _workspace(workspace: Optional[torch.Tensor], device: int):
@@ -592,11 +592,20 @@ def moe_expert_ffn_backward(shape: MoeShape, weights: MoeWeights, x_perm, expert
 
 
 class Block:
-    """What stands at the end of a block: its numbers, and the tensors that hold its weights."""
+    """What stands at the end of a block: its numbers, and the tensors that hold its weights.  Their sizes and device are
+    looked at once, here."""
 
     def __init__(self, struct: BlockStruct, tensors: Dict[str, Optional[torch.Tensor]]):
         self.struct, self.tensors = struct, tensors
-        self.held = [(name, t) for name, t in tensors.items() if t is not None]
+        held = [t for t in tensors.values() if t is not None]
+        if held:
+            _same_device(*held)
+        self.device = held[0].get_device() if held else None
+        widths = {t.shape[0] for t in (tensors["post_w"], tensors["gate"]) if t is not None}
+        if len(widths) > 1:
+            raise ValueError(f"post_w and gate of {sorted(widths)} values")
+        self.width = min(widths, default=None)
+        self.tokens = None if tensors["token_gate"] is None else tensors["token_gate"].shape[0]
 
 
 def make_block(eps=1e-5, skip_scale=1.0, block_scale=1.0, dropout=0.0, post_w=None, gate=None, token_gate=None, rng=None) -> Block:
@@ -621,12 +630,13 @@ def alloc_block_workspace(n_tokens: int, d_model: int, device) -> torch.Tensor:
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 
-def _block_check(block: Block, T: int, d: int, device: int, weights: bool) -> None:
-    for name, v in block.held:
-        if weights and name != "rng" and v.shape[0] != (T if name == "token_gate" else d):
-            raise ValueError(f"{name} must have {T if name == 'token_gate' else d} values, got {v.shape[0]}")
-        if v.get_device() != device:
-            raise ValueError(f"the block's {name} on another device than the call's first tensor")
+def _block_check(block: Block, T: int, d: int, device: int, used: bool) -> None:
+    if block.device is not None and block.device != device:
+        raise ValueError("the block's tensors on another device than the call's first tensor")
+    if used and block.width is not None and block.width != d:
+        raise ValueError(f"post_w and gate must have {d} values, got {block.width}")
+    if used and block.tokens is not None and block.tokens != T:
+        raise ValueError(f"token_gate must have {T} values, got {block.tokens}")
 
 
 def moe_block_norm(block: Block, x, b, open_w, y, n) -> None:

@@ -223,6 +223,8 @@ def test_binding_refuses():
     with pytest.raises(ValueError):
         pkg.moe_block_norm(pkg.make_block(post_w=t(24)), t(3, 16), t(3, 16), None, t(3, 16), None)
     with pytest.raises(ValueError):
+        pkg.make_block(post_w=t(16), gate=t(24))
+    with pytest.raises(ValueError):
         pkg.moe_block_norm(pkg.make_block(token_gate=t(4)), t(3, 16), t(3, 16), None, t(3, 16), None)
     with pytest.raises(ValueError):
         pkg.moe_block_stack_forward(shape, [pkg.MoeWeights()], [], [], t(3, 16), t(3, 16))
