@@ -53,6 +53,16 @@ __device__ __forceinline__ bf16x8 read_transposed(unsigned at, unsigned rows4) {
 #endif
 }
 
+// A fragment's eight k-values from k on, those from `left` on as zeros.  (Two to a register: value by value it was a third of all vector
+// instructions of a tile of few steps.)
+__device__ __forceinline__ bf16x8 first_of(bf16x8 v, int k, int left) {
+    typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+    u32x4 u = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) u[j] &= k + 2 * j + 1 < left ? ~0u : k + 2 * j < left ? 0xFFFFu : 0u;
+    return __builtin_bit_cast(bf16x8, u);
+}
+
 // BM, COLS: rows and output columns of a tile (DX, WEIGHTS: 256 columns)
 template <int OP, int BM, int COLS>
 struct Form {
@@ -265,11 +275,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                 const int ks = KS == 2 ? phase : q;
                 if constexpr (WGT) {  // they are the last ones
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const bool past = ks * 32 + (lane >> 4) * 8 + j >= left;
-#pragma unroll
-                        for (int mi = 0; mi < 2 * MA; ++mi) fa[q][mi][j] = past ? (bf16_t)0.f : fa[q][mi][j];
-                    }
+                    for (int mi = 0; mi < 2 * MA; ++mi) fa[q][mi] = first_of(fa[q][mi], ks * 32 + (lane >> 4) * 8, left);
                 } else if (ks * 32 + (lane >> 4) * 8 < BK - left) {  // they are the first ones (a multiple of 8)
 #pragma unroll
                     for (int mi = 0; mi < 2 * MA; ++mi) fa[q][mi] = bf16x8{};
@@ -532,11 +538,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         for (int ni = 0; ni < 8; ++ni) fb[ni] = read_transposed(pb + (((unsigned)(wn * 8 + ni) << 5) ^ swz), 4 * 512);
         if (v == nk - 1 && K % kWgtK) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const bool past = (lane >> 4) * 8 + j >= K - v * kWgtK;
-#pragma unroll
-                for (int mi = 0; mi < 4; ++mi) fa[mi][j] = past ? (bf16_t)0.f : fa[mi][j];
-            }
+            for (int mi = 0; mi < 4; ++mi) fa[mi] = first_of(fa[mi], (lane >> 4) * 8, K - v * kWgtK);
         }
 #pragma unroll
         for (int ni = 0; ni < 8; ++ni)
