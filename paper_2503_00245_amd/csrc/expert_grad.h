@@ -42,7 +42,6 @@ int run_grad_plain(const GradArgs& g, GradOp op, int act_dtype, hipStream_t st);
 
 // bf16 (expert_grad_mfma.hip)
 bool grad_mfma_supported(const GradArgs& g);
-size_t grad_parts_bytes(long long P, int d);  // of GradArgs::parts
 int run_grad_mfma(const GradArgs& g, GradOp op, hipStream_t st);
 
 }  // namespace moe

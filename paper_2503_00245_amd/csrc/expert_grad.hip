@@ -6,6 +6,7 @@
 //
 // The kernels here: tiles of 64 x 64 on four waves, operands widened to fp32 in LDS, v_mfma_f32_16x16x4_f32.
 #include "expert_grad.h"
+#include "expert_grad_plan.h"
 
 namespace moe {
 
@@ -199,10 +200,11 @@ GradLayout grad_layout(const moe_shape& s) {
 int validate_grad(const moe_shape* s) {
     const int rc = validate_shape(s);
     if (rc != MOE_OK) return rc;
-    // tiles of a launch are counted in 31 bits
+    // a launch has fewer than 2^32 threads: tiles of 64 by 64 of the rows' products, strips of 256 hidden columns by tiles across d of the weights'
     const long long tiles_d = (s->d_model + TILE - 1) / TILE, tiles_f = (s->d_ff + TILE - 1) / TILE;
     const long long rows = ((long long)s->n_tokens * s->top_k + TILE - 1) / TILE + s->n_experts;
-    if (s->rank != 0 || s->d_model > (1 << 18) || s->d_ff > (1 << 18) || tiles_d * tiles_f >= (1 << 23) || rows * (tiles_d > tiles_f ? tiles_d : tiles_f) >= (1 << 23))
+    if (s->rank != 0 || s->d_model > (1 << 18) || s->d_ff > (1 << 18) || tiles_d * tiles_f >= (1 << 23) || rows * (tiles_d > tiles_f ? tiles_d : tiles_f) >= (1 << 23) ||
+        (s->n_experts * 3ll * ((s->d_ff + 255) / 256) + 8) * 2 * ((s->d_model + 255) / 256) >= (1 << 23))
         return MOE_ERR_UNSUPPORTED;
     return MOE_OK;
 }

@@ -18,10 +18,10 @@
 // accumulator registers a lane) or 96 (144), a and b in a first pass over d, dh in a second one.  dh then is never rounded nor
 // stored: as a tensor of its own in bf16 it raised the error of the gradients from 2.4e-3 to 2.9e-3.
 #include "expert_grad.h"
+#include "expert_grad_plan.h"
 #include "lds_fill.h"
 
 #include <algorithm>
-#include <cmath>
 
 namespace moe {
 
@@ -460,9 +460,6 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 // workgroups share a CU, one's stores beside the other's products: tiles of 128 x 256 on four waves, k-steps of 32 rows, three of them in
 // LDS, one barrier a step.  A and B lie as in grad_kernel (A's rows of 256 bytes).
 constexpr int kWgtM = 128, kWgtN = 256, kWgtK = 32, kWgtStages = 3;
-// Rows of an expert, on average, below which (256 x 256 / these, us: 24 tokens of 1024 / 2816, 4 of 16 experts, 80 / 53, 777 of 1440 / 3840 117 / 99,
-// 2048 of 2048 / 5632 362 / 371, 16384 1675 / 1895)
-constexpr int kWgtSmallRows = 384;
 constexpr int kWgtA = kWgtM * kWgtK * 2, kWgtStage = (kWgtM + kWgtN) * kWgtK * 2, kWgtLds = kWgtStages * kWgtStage;
 
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void grad_weights_small_kernel(const GradArgs g) {
@@ -583,34 +580,6 @@ int launch(const GradArgs& g, int grid, hipStream_t st) {
 // A pass has as many k-steps as are fetched ahead of the first.  (Offsets within a tile, of 256 rows of at most 2^18 values, are 32 bits.)
 bool grad_mfma_supported(const GradArgs& g) { return g.d > 2 * BK && g.F > 2 * BK; }
 
-// Row tiles that a layer's groups are expected to need: beside whole ones about half a tile each, a little more as loads are uneven
-static double tiles_expected(const GradArgs& g, int bm) {
-    const double groups = std::min(g.P, g.E);
-    return std::max(groups, (double)g.P / bm + 0.6 * groups);
-}
-
-// ---- gx in parts --------------------------------------------------------------------------------------
-// Its tiles are few (rows by d, where the other products have F or F by d) and long (2 F deep).  Where they do not fill the CUs their k-steps are cut
-// into up to four runs, summed by a launch of its own in fp32.  A model of the launch in us decides: rounds of 256 workgroups (the last
-// one of halves where that does), 1.15 us a step of full tiles, 0.8 of near empty ones, 8 us beside the steps, and the sums at 4.5 TB/s.
-size_t grad_parts_bytes(long long P, int d) {  // room for them; does not fall as P grows
-    return std::min<size_t>(16 * (size_t)P * d, 200u << 20);
-}
-int grad_parts(const GradArgs& g) {
-    const double groups = std::min(g.P, g.E), tiles = tiles_expected(g, 256) * ((g.d + 255) / 256);
-    const double step = std::max(0.8, 1.15 * std::min(1.0, g.P / groups / 192)), steps = 2 * ((g.F + BK - 1) / BK);
-    const int most = (int)std::min<size_t>(4, grad_parts_bytes(g.P, g.d) / (4 * (size_t)g.P * g.d));
-    int best = 1;
-    double best_cost = 0;
-    for (int q = 1; q <= most && steps / q >= 8; ++q) {
-        double rounds = tiles * q / 256;
-        rounds = rounds <= 1 ? 1 : std::ceil(2 * rounds) / 2;
-        const double cost = rounds * (steps / q * step + 8) + (q > 1 ? 6 + 4.0 * q * g.P * g.d / 4.5e6 : 0);
-        if (q == 1 || cost < best_cost) best = q, best_cost = cost;
-    }
-    return best;
-}
-
 // gx = the sum of its parts, in order, rounded once; rows of no group stay as they are
 __global__ __launch_bounds__(256) void sum_grad_parts_kernel(const float* __restrict__ parts, int q, const int32_t* __restrict__ offsets, int E, int P, int d,
                                                              bf16_t* __restrict__ gx) {
@@ -629,36 +598,30 @@ __global__ __launch_bounds__(256) void sum_grad_parts_kernel(const float* __rest
 }
 
 int run_grad_mfma(const GradArgs& g, GradOp op, hipStream_t st) {
+    const GradPlan plan = grad_plan(g.P, g.E, g.d, g.F);
     if (op == GRAD_WEIGHTS) {
-        const int strips = g.E * 3 * ((g.F + 255) / 256);
-        if (g.P < (long long)kWgtSmallRows * g.E) {
-            static std::atomic<uint64_t> lds_allowed;
-            if (allow_dynamic_lds(reinterpret_cast<const void*>(grad_weights_small_kernel), kWgtLds, lds_allowed) != MOE_OK) return MOE_ERR_LAUNCH;
-            hipLaunchKernelGGL(grad_weights_small_kernel, dim3((strips + 7) / 8 * 8 * 2 * ((g.d + 255) / 256)), dim3(256), kWgtLds, st, g);
-            return launch_status();
-        }
-        return launch<GRAD_WEIGHTS, 256, 256, false>(g, (strips + 7) / 8 * 8 * ((g.d + 255) / 256), st);
+        const int strips = (g.E * 3 * ((g.F + 255) / 256) + 7) / 8 * 8, across = (g.d + 255) / 256;
+        if (!plan.small_weights) return launch<GRAD_WEIGHTS, 256, 256, false>(g, strips * across, st);
+        static std::atomic<uint64_t> lds_allowed;
+        if (allow_dynamic_lds(reinterpret_cast<const void*>(grad_weights_small_kernel), kWgtLds, lds_allowed) != MOE_OK) return MOE_ERR_LAUNCH;
+        hipLaunchKernelGGL(grad_weights_small_kernel, dim3(strips * across * 2), dim3(256), kWgtLds, st, g);
+        return launch_status();
     }
     if (op == GRAD_ACT) {
-        // 256 rows by 128 columns take 1.21 times as long as by 96, 128 rows by 128 0.72 times; whole rounds decide, and near empty
-        // tiles are bound by the weights (us, 256 x 96 / 256 x 128 / 128 x 128: 24 tokens of 1024 / 2816, 4 of 16 experts, 57 / 70 / 59, 777 of 1440 / 3840
-        // 133 / 140 / 114, 2048 of 2048 / 5632 353 / 346 / 363, 16384 2365 / 2140 / 2380)
-        auto tiles = [&](int bm, int cols) { return m_tiles_bound(g.P, g.E, bm) * ((g.F + cols - 1) / cols); };
-        auto cost = [&](int bm, int cols, double tile) { return tile * std::ceil(tiles_expected(g, bm) * ((g.F + cols - 1) / cols) / 256); };
-        const double wide = cost(256, 128, 1.21), narrow = cost(256, 96, 1.0), low = cost(128, 128, 0.72);
-        if (low < wide && low < narrow && g.P > 32ll * g.E && g.d > 3 * BK) return launch<GRAD_ACT, 128, 128, false>(g, find_tile_grid(tiles(128, 128), kSplitSlots), st);
-        if (wide < narrow) return launch<GRAD_ACT, 256, 128, false>(g, find_tile_grid(tiles(256, 128), kSplitSlots), st);
-        return launch<GRAD_ACT, 256, 96, false>(g, find_tile_grid(tiles(256, 96), kSplitSlots), st);
+        const int grid = find_tile_grid(m_tiles_bound(g.P, g.E, plan.act_rows) * ((g.F + plan.act_cols - 1) / plan.act_cols), kSplitSlots);
+        return plan.act_rows == 128   ? launch<GRAD_ACT, 128, 128, false>(g, grid, st)
+               : plan.act_cols == 128 ? launch<GRAD_ACT, 256, 128, false>(g, grid, st)
+                                      : launch<GRAD_ACT, 256, 96, false>(g, grid, st);
     }
-    const int tiles = m_tiles_bound(g.P, g.E, 256) * ((g.d + 255) / 256), parts = grad_parts(g);
-    if (parts == 1) return launch<GRAD_DX, 256, 256, false>(g, find_tile_grid(tiles, kSplitSlots), st);
+    const int grid = find_tile_grid(m_tiles_bound(g.P, g.E, 256) * ((g.d + 255) / 256) * plan.dx_parts, kSplitSlots);
+    if (plan.dx_parts == 1) return launch<GRAD_DX, 256, 256, false>(g, grid, st);
     GradArgs cut = g;
-    cut.k_parts = parts;
-    const int rc = launch<GRAD_DX, 256, 256, true>(cut, find_tile_grid(tiles * parts, kSplitSlots), st);
+    cut.k_parts = plan.dx_parts;
+    const int rc = launch<GRAD_DX, 256, 256, true>(cut, grid, st);
     if (rc != MOE_OK) return rc;
     const long long chunks = (long long)g.P * g.d / 8;
-    hipLaunchKernelGGL(sum_grad_parts_kernel, dim3((unsigned)std::min<long long>((chunks + 255) / 256, 2048)), dim3(256), 0, st, g.parts, parts, g.offsets, g.E,
-                       g.P, g.d, static_cast<bf16_t*>(g.gx));
+    hipLaunchKernelGGL(sum_grad_parts_kernel, dim3((unsigned)std::min<long long>((chunks + 255) / 256, 2048)), dim3(256), 0, st, g.parts, cut.k_parts,
+                       g.offsets, g.E, g.P, g.d, static_cast<bf16_t*>(g.gx));
     return launch_status();
 }
 

@@ -31,7 +31,7 @@ def block_of(cfg):
     return pkg.make_block(**{n: on(v) if torch.is_tensor(v) else v for n, v in cfg.items()})
 
 
-SHAPES = [(1, 8), (1, 2048), (3, 40), (17, 512), (5, 520), (130, 432), (2049, 1440), (2500, 64), (3, 8192), (2, 8200), (1, 32768), (600, 2056)]
+SHAPES = [(1, 8), (1, 2048), (3, 40), (17, 512), (5, 520), (130, 432), (2049, 1440), (2500, 64), (3, 8192), (2, 8200), (1, 32768), (600, 2056), (210, 8200)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -86,6 +86,55 @@ def test_block(T, d, what, dtype):
         pkg.moe_block_norm_backward(blk, on(u), on(gn), y, None, on(w), gx, None, gw, workspace=ws)
         to.near(gx, want["x"], "x alone")
         to.near(gw, want["open_w"], "open_w alone")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,d", [(17001, 40), (4501, 520), (9001, 1032), (4500, 2056), (4200, 4104), (4105, 8200)])
+def test_rows_do_not_depend_on_the_rows_around_them(T, d, dtype):
+    # workgroups that take many rows in turn give every row what a call of a few rows gives it, bit for bit
+    dt = DTYPES[dtype]
+    g = torch.Generator(device=dev())
+    g.manual_seed(T)
+    rows = lambda: torch.randn(T, d, generator=g, device=dev()).to(dt)  # noqa: E731
+    x, b, gy, gn = rows(), rows(), rows(), rows()
+    w = [1 + torch.randn(d, generator=g, device=dev()) * 0.2 for _ in range(3)]
+    tg = torch.rand(T, generator=g, device=dev())
+
+    def run(at, sums):
+        blk = pkg.make_block(skip_scale=0.5, block_scale=2.0, post_w=w[0], gate=w[1], token_gate=tg[at].contiguous())
+        n = tg[at].shape[0]
+        y, no, gx, gb = (torch.full((n, d), float("nan"), dtype=dt, device=dev()) for _ in range(4))
+        gt = torch.full((n,), float("nan"), device=dev())
+        pkg.moe_block_norm(blk, x[at], b[at], w[2], y, no)
+        parts = [torch.empty(d, device=dev()) for _ in range(3)] if sums else [None] * 3
+        pkg.moe_block_norm_backward(blk, gy[at], gn[at], y, b[at], w[2], gx, gb, *parts, gt, pkg.alloc_block_workspace(n, d, dev()) if sums else None)
+        return [y, no, gx, gb, gt]
+    whole, bare = run(slice(0, T), True), run(slice(0, T), False)
+    assert all(torch.equal(p, q) for p, q in zip(whole, bare))
+    for lo in [*range(0, T, T // 7), T - 3]:
+        few = run(slice(lo, min(lo + 50, T)), False)
+        assert all(torch.equal(p[lo:lo + 50], q) for p, q in zip(whole, few))
+
+
+def test_rows_beyond_32_bit_offsets():
+    # 2^21 + 3 rows of 2056 values: over 2^32 values a tensor; rows as calls of a few rows give them
+    T, d = (1 << 21) + 3, 2056
+    g = torch.Generator(device=dev())
+    g.manual_seed(6)
+    x = torch.randint(-9, 9, (T, d), generator=g, device=dev(), dtype=torch.int8).bfloat16()
+    blk = pkg.make_block(post_w=torch.rand(d, generator=g, device=dev()))
+    y, n = torch.empty_like(x), torch.empty_like(x)
+    w = torch.rand(d, generator=g, device=dev())
+    pkg.moe_block_norm(blk, x, x, w, y, n)
+    at = slice(T - 40, T)
+    y1, n1 = torch.empty_like(x[at]), torch.empty_like(x[at])
+    pkg.moe_block_norm(blk, x[at], x[at], w, y1, n1)
+    assert torch.equal(y[at], y1) and torch.equal(n[at], n1)
+    gx, gb = torch.empty_like(x), n  # (n is not needed any more)
+    pkg.moe_block_norm_backward(blk, x, None, None, y, None, gx, gb)
+    gx1, gb1 = torch.empty_like(y1), torch.empty_like(y1)
+    pkg.moe_block_norm_backward(blk, x[at], None, None, y1, None, gx1, gb1)
+    assert torch.equal(gx[at], gx1) and torch.equal(gb[at], gb1)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])

@@ -3,13 +3,18 @@ that the GPU tests compare with, against automatic differentiation and against d
 import ctypes as C
 import os
 import re
+import subprocess
 
 import numpy as np
 import pytest
 import torch
 
 import paper_2503_00245_amd as pkg
+from paper_2503_00245_amd import build as hip_build
 from tests import training_oracle as to
+from tests.training_cases import EXPERTS as LAYERS
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 INVALID, UNSUPPORTED, WORKSPACE = -1, -2, -3
 P = [C.c_void_p(i << 20) for i in range(1, 20)]  # addresses that no launch will see
@@ -20,8 +25,7 @@ BIG = 1 << 40
 
 
 def test_header_binding_and_library_agree():
-    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
-    names = re.findall(r"MOE_API\s+[\w\s\*]+?\b(moe_\w+)\s*\(", open(os.path.join(root, "include", "moe_training.h")).read())
+    names = re.findall(r"MOE_API\s+[\w\s\*]+?\b(moe_\w+)\s*\(", open(os.path.join(ROOT, "include", "moe_training.h")).read())
     assert set(names) == set(pkg.TRAINING_EXPORTS)
     for n in names:
         assert getattr(pkg.lib(), n) is not None
@@ -113,7 +117,7 @@ def test_gradient_of_experts_refuses():
     assert call(fn, EXPERTS, gx=None, gg=None, gu=None, gd=None) == 0
     assert call(fn, EXPERTS, shape=pkg.make_shape(0, 64, 136, 4, 2), x=None, off=None, gy=None, gg=None, gu=None, gd=None) == 0
     for bad in (dict(rank=8), dict(d_ff=(1 << 18) + 8), dict(d_model=(1 << 18) + 8), dict(d_model=1 << 18, d_ff=1 << 18),
-                dict(n_tokens=1 << 22, d_ff=1 << 14)):
+                dict(n_tokens=1 << 22, d_ff=1 << 14), dict(n_experts=64, d_model=1 << 16, d_ff=1 << 16)):
         shape = pkg.make_shape(**dict(dict(n_tokens=8, d_model=64, d_ff=136, n_experts=4, top_k=2), **bad))
         assert call(fn, EXPERTS, shape=shape) == UNSUPPORTED, bad
         assert pkg.moe_training_workspace_bytes(shape) == 0
@@ -246,6 +250,16 @@ def test_binding_refuses_host_tensors():
     for call_ in calls:
         with pytest.raises(ValueError, match="GPU"):
             call_()
+
+
+def test_the_tested_layers_reach_every_tile_of_the_experts_gradient(tmp_path):
+    exe = str(tmp_path / "check")
+    subprocess.run(["g++", "-O2", "-std=c++17", "-I", hip_build.CSRC, os.path.join(ROOT, "tests", "expert_grad_plan_check.cpp"), "-o", exe], check=True)
+    plans = [tuple(map(int, subprocess.run([exe, str(T * k), str(E), str(d), str(F)], capture_output=True, text=True, check=True, timeout=60).stdout.split()))
+             for T, d, F, E, k in LAYERS if d > 128 and F > 128]  # (narrower layers take the kernels for any size)
+    assert {p[:2] for p in plans} == {(256, 96), (256, 128), (128, 128)}
+    assert {p[2] for p in plans} == {1, 2, 3, 4}
+    assert {p[3] for p in plans} == {0, 1}
 
 
 # ---- the plain implementations themselves ---------------------------------------------------------------------------

@@ -5,6 +5,7 @@ import torch
 
 import paper_2503_00245_amd as pkg
 from tests import training_oracle as to
+from tests.training_cases import EXPERTS
 
 pytestmark = pytest.mark.gpu
 DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
@@ -114,6 +115,46 @@ def test_collect_and_its_gradient(T, d, E, k, dtype):
         assert torch.equal(place, gY) and torch.equal(only, gg)
 
 
+def test_rows_of_many_pairs():
+    # 12 million pairs of 64 experts: chunks of thousands of tokens, many passes each
+    T, E, k = 3_000_001, 64, 4
+    g = torch.Generator(device=dev())
+    g.manual_seed(2)
+    shape, ws = make(T, 8, E, k, torch.float32)
+    idx = torch.randint(-1, E, (T, k), generator=g, device=dev(), dtype=torch.int32)
+    x = torch.randn(T, 8, generator=g, device=dev())
+    off, perm, inv, rows = dispatched(shape, idx, None, x, ws)
+    key = torch.where(idx.flatten() < 0, E, idx.flatten())
+    order = torch.argsort(key, stable=True)
+    live = int((key < E).sum())
+    assert off.tolist() == [int((key < e).sum()) for e in range(E + 1)]
+    assert torch.equal(perm[:live].long(), order[:live]) and (perm[live:] == -1).all()
+    assert torch.equal(inv.long()[order[:live]], torch.arange(live, device=dev())) and (inv[key == E] == -1).all()
+    assert torch.equal(rows[:live], x[order[:live] // k]) and (rows[live:] == 0).all()
+
+
+def test_rows_beyond_32_bit_offsets():
+    # 2^21 + 2 rows of 2056 values: over 2^32 values a tensor
+    T, d, E, k = (1 << 20) + 1, 2056, 3, 2
+    g = torch.Generator(device=dev())
+    g.manual_seed(4)
+    shape, ws = make(T, d, E, k, torch.bfloat16)
+    idx = torch.randint(0, E, (T, k), generator=g, device=dev(), dtype=torch.int32)
+    x = torch.randint(-8, 8, (T, d), generator=g, device=dev(), dtype=torch.int8).bfloat16()
+    off, perm, inv, rows = dispatched(shape, idx, None, x, ws)
+    at = torch.cat([torch.arange(0, T * k, 5003, device=dev()), torch.tensor([T * k - 1], device=dev())])
+    assert torch.equal(rows[at], x[perm[at].long() // k])
+    t = perm[at].long() // k
+    gate = torch.ones(T, k, device=dev())
+    y = torch.empty_like(x)
+    pkg.moe_collect(shape, rows, inv, gate, None, y)
+    assert torch.equal(y[t], 2 * x[t])  # two rows of the same token, exact in bf16
+    gg = torch.empty(T, k, device=dev())
+    pkg.moe_collect_backward(shape, x, rows, off, inv, gate, rows, gg)  # the gradient in place of the rows, which it equals here
+    assert torch.equal(rows[at], x[t])
+    assert torch.equal(gg[t], x[t].float().square().sum(-1, keepdim=True).expand(-1, k))  # sums of whole numbers under 2^24: exact
+
+
 def test_the_same_expert_twice_and_rows_outside():
     # a token that names one expert twice has two rows; values of inv_perm outside the rows are pairs without one
     shape, ws = make(3, 16, 4, 2, torch.float32)
@@ -146,10 +187,6 @@ def _backward(shape, ws, offsets, x, gy, w, which=(1, 1, 1, 1)):
     outs = [torch.full_like(t, float("nan")) if on else None for t, on in zip([x] + w, which)]
     pkg.moe_expert_ffn_backward(shape, weights, x, offsets, gy, *outs, ws)
     return outs
-
-
-EXPERTS = [(1, 8, 8, 1, 1), (1, 40, 72, 4, 2), (5, 64, 136, 8, 3), (33, 128, 128, 2, 1), (7, 136, 136, 4, 2), (24, 256, 512, 16, 4), (40, 432, 1152, 8, 2),
-           (100, 328, 264, 3, 2), (777, 160, 200, 8, 2), (1500, 264, 520, 4, 1), (64, 520, 1064, 64, 6), (300, 1440, 456, 4, 2), (2, 2048, 256, 8, 2)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
