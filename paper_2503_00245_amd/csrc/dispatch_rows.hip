@@ -1,7 +1,9 @@
 // Tokens to rows sorted by expert and back, with weights, and the gradients of both (moe_training.h states them).
 //
-// All four move rows and little else: what bounds them is memory.  A token's row is read once for all of its pairs, or
+// All four move rows and little else: what bounds them is memory, or the launch.  A token's row is read once for all of its pairs, or
 // written once from all of them, 16 bytes a lane; dot products for the weights are formed from the values that pass by.
+// 16384 tokens of 2048, two of 8 experts, bf16, in a graph: dispatch 36.8 us (196 MB, 5.3 TB/s), collect 29.5 (201 MB, 6.8 TB/s, part of it from the
+// memory-side cache), its gradient 63-66 (336 MB, 5.1-5.3 TB/s); a copy of 1 GiB moves 5.1 TB/s both ways together.
 #include <algorithm>
 
 #include "moe_training.h"
@@ -13,7 +15,9 @@ namespace {
 
 constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / kWave;
-constexpr int kKeysAlone = 4096;   // pairs up to which every workgroup counts all keys itself
+// Pairs up to which every workgroup counts all keys itself, and counting needs no launch of its own (us, so / with that launch: 96 pairs of 16 experts
+// 5.6 / 8.1, 2048 pairs of 8 6.8 / 8.8, 4096 of 8 10.0 / 10.7, of 64 8.2 / 11.8, 8192 of 64 11.6 / 14.0, of 8 15.2 / 13.9, 16384 of 8 20.2 / 14.3)
+constexpr int kKeysAlone = 8192;
 constexpr int kMaxCounts = 16384;  // counts that a workgroup adds up beyond
 
 // Chunks of whole tokens: about two workgroups a CU, no more chunks than their counts may be
@@ -70,11 +74,22 @@ __global__ __launch_bounds__(kThreads) void dispatch_kernel(ptr_arg a_keys, ptr_
     for (int i = threadIdx.x; i <= E; i += kThreads) s_all[i] = s_run[i] = 0;
     __syncthreads();
     if (counts) {
-        const int n = gridDim.x * E;
-        for (int i = threadIdx.x; i < n; i += kThreads) {
-            const int c = quick_div(i, E), e = i - c * E, v = counts[i];
-            atomicAdd(&s_all[e], v);
-            if (c < (int)blockIdx.x) atomicAdd(&s_run[e], v);
+        // (a thread sums chunks of one expert and adds once: an addition in LDS for every count was 10 us of 64 experts)
+        const int per = kThreads / E, c0 = quick_div(threadIdx.x, E), e = (int)threadIdx.x - c0 * E;
+        if (c0 < per) {
+            int all = 0, before = 0;
+            for (int c = c0; c < (int)gridDim.x; c += 8 * per) {  // eight loads in flight
+                int v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = c + j * per < (int)gridDim.x ? counts[(c + j * per) * E + e] : 0;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    all += v[j];
+                    before += c + j * per < (int)blockIdx.x ? v[j] : 0;
+                }
+            }
+            atomicAdd(&s_all[e], all);
+            atomicAdd(&s_run[e], before);
         }
     } else {
         for (int p = threadIdx.x; p < P; p += kThreads) {
@@ -168,11 +183,10 @@ __global__ __launch_bounds__(kThreads) void dispatch_kernel(ptr_arg a_keys, ptr_
 }
 
 // ---- rows to tokens --------------------------------------------------------------------------------------
-// WAVES of a workgroup share a token: one where tokens fill the chip, four where a call's latency counts.  K: pairs of a token held
-// in registers, 0: any number, their dot products in LDS.
+// WAVES of a workgroup of four share a token, by its width.  K: pairs of a token held in registers, 0: any number, their dot
+// products in LDS.
 template <int WAVES, int K>
 struct Dots {
-    static constexpr int kTokens = 4 / WAVES;
     float* lds;   // [k][64] of this wave (K == 0)
     float v[K ? K : 1];
     __device__ __forceinline__ void clear(int k, int lane) {
@@ -206,7 +220,12 @@ struct Dots {
         }
         if (WAVES > 1) {
             __syncthreads();
-            if (wave == 0 && lane < k && valid) out[lane] = (s_part[0][lane] + s_part[1][lane]) + (s_part[2][lane] + s_part[3][lane]);
+            if (wave % WAVES == 0 && lane < k && valid) {
+                f32x4 sum{};
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) sum[w] = s_part[wave + w][lane];
+                out[lane] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            }
         }
     }
 };
@@ -224,9 +243,10 @@ __global__ __launch_bounds__(256) void collect_kernel(ptr_arg a_inv, ptr_arg a_w
     extern __shared__ float s_dots[];
     __shared__ float s_part[4][kWave];
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const int t = WAVES == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
+    const int t = blockIdx.x * (4 / WAVES) + wave / WAVES;
     const bool valid = t < n_tokens;
     if (WAVES == 1 && !valid) return;
+    if (!valid) d = 0;  // (the waves of a token that is not there come to the barrier)
     Dots<WAVES, K> dot;
     dot.lds = s_dots + wave * k * kWave;
     if (DOTS) dot.clear(k, lane);
@@ -236,11 +256,11 @@ __global__ __launch_bounds__(256) void collect_kernel(ptr_arg a_inv, ptr_arg a_w
     float g[K ? K : 1];
 #pragma unroll
     for (int j = 0; j < K; ++j) {
-        row[j] = j < k ? inv[j] : -1;
-        g[j] = j < k && w ? w[j] : 1.f;
+        row[j] = j < k && valid ? inv[j] : -1;
+        g[j] = j < k && valid && w ? w[j] : 1.f;
         if ((unsigned)row[j] >= (unsigned)P) row[j] = -1;
     }
-    for (int c = ((WAVES == 1 ? 0 : wave * kWave) + lane) * 8; c < d; c += WAVES * kWave * 8) {
+    for (int c = (wave % WAVES * kWave + lane) * 8; c < d; c += WAVES * kWave * 8) {
         float acc[8];
         Raw8<T> xv{}, res{};
         if (DOTS) xv = load8(x + (size_t)t * d + c);
@@ -292,13 +312,15 @@ __global__ __launch_bounds__(256) void spread_kernel(ptr_arg a_inv, ptr_arg a_ga
     extern __shared__ float s_dots[];
     __shared__ float s_part[4][kWave];
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const int t = WAVES == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
+    const int t = blockIdx.x * (4 / WAVES) + wave / WAVES;
+    const bool valid = t < n_tokens;
     if (ROWS) {
         const float zero[8] = {};
         for (int s = max(offsets[E], 0) + (int)blockIdx.x * 4 + wave; s < P; s += gridDim.x * 4)
             for (int c = lane * 8; c < d; c += kWave * 8) store8(grad_rows + (size_t)s * d + c, round8<T>(zero));
     }
-    if (WAVES == 1 && t >= n_tokens) return;
+    if (WAVES == 1 && !valid) return;
+    if (!valid) d = 0;
     Dots<WAVES, K> dot;
     dot.lds = s_dots + wave * k * kWave;
     if (DOTS) dot.clear(k, lane);
@@ -308,11 +330,11 @@ __global__ __launch_bounds__(256) void spread_kernel(ptr_arg a_inv, ptr_arg a_ga
     float g[K ? K : 1];
 #pragma unroll
     for (int j = 0; j < K; ++j) {
-        row[j] = j < k ? inv[j] : -1;
-        g[j] = ROWS && j < k ? w[j] : 0.f;
+        row[j] = j < k && valid ? inv[j] : -1;
+        g[j] = ROWS && valid && j < k ? w[j] : 0.f;
         if ((unsigned)row[j] >= (unsigned)P) row[j] = -1;
     }
-    for (int c = ((WAVES == 1 ? 0 : wave * kWave) + lane) * 8; c < d; c += WAVES * kWave * 8) {
+    for (int c = (wave % WAVES * kWave + lane) * 8; c < d; c += WAVES * kWave * 8) {
         const Raw8<T> up = load8(gy + (size_t)t * d + c);
         auto pair = [&](int j, int s, float f, const Raw8<T>& v) {
             float sum = 0.f, o[8];
@@ -342,34 +364,34 @@ __global__ __launch_bounds__(256) void spread_kernel(ptr_arg a_inv, ptr_arg a_ga
             }
         }
     }
-    if (DOTS) dot.finish(k, lane, wave, s_part, dots + (size_t)t * k, true);
+    if (DOTS) dot.finish(k, lane, wave, s_part, dots + (size_t)t * k, valid);
 }
 
 constexpr size_t kDotsLds = sizeof(float) * 4 * kWave * kMaxExperts;  // dot products of 64 pairs, a sum per lane
 
-// Tokens from which one wave each takes them
-constexpr int kWaveTokens = 2048;
-
+// A wave for every 512 values, up to four (us, one wave / four / so: collect of 16384 tokens of 432, two experts, 7.8 / 9.6 / 7.8, 2048 of 2048 4.8 / 4.1 / 4.2;
+// its gradient at 16384 of 2048 68.0 / 65.0 / 62.8, 8192 of 1024 14.4 / 15.6 / 14.7, 2048 of 720, eight experts, 11.5 / 13.6 / 10.4)
 template <typename F>
-int by_size(int T, int k, F run) {
+int by_size(int d, int k, F run) {
     typedef std::integral_constant<int, 1> one;
+    typedef std::integral_constant<int, 2> two;
     typedef std::integral_constant<int, 4> four;
     auto on = [&](auto waves) {
-        if (k == 1) return run(waves, std::integral_constant<int, 1>{});
-        if (k == 2) return run(waves, std::integral_constant<int, 2>{});
-        if (k <= 4) return run(waves, std::integral_constant<int, 4>{});
+        if (k == 1) return run(waves, one{});
+        if (k == 2) return run(waves, two{});
+        if (k <= 4) return run(waves, four{});
         if (k <= 8) return run(waves, std::integral_constant<int, 8>{});
         return run(waves, std::integral_constant<int, 0>{});
     };
-    return T >= kWaveTokens ? on(one{}) : on(four{});
+    return d <= 512 ? on(one{}) : d <= 1024 ? on(two{}) : on(four{});
 }
 
 template <typename T>
 int run_collect(const moe_shape& s, const void* rows, const int32_t* inv, const float* weight, const void* residual, const void* x, void* out,
                 float* dots, hipStream_t st) {
-    return by_size(s.n_tokens, s.top_k, [&](auto waves, auto kk) {
+    return by_size(s.d_model, s.top_k, [&](auto waves, auto kk) {
         constexpr int W = decltype(waves)::value, K = decltype(kk)::value;
-        const int grid = W == 1 ? (s.n_tokens + 3) / 4 : s.n_tokens;
+        const int grid = (s.n_tokens + 4 / W - 1) / (4 / W);
         const size_t lds = K == 0 && dots ? sizeof(float) * 4 * kWave * s.top_k : 0;
         const auto kern = dots ? collect_kernel<T, W, K, true> : collect_kernel<T, W, K, false>;
         static std::atomic<uint64_t> lds_allowed;
@@ -384,9 +406,9 @@ template <typename T>
 int run_spread(const moe_shape& s, const void* gy, const void* rows, const int32_t* offsets, const int32_t* inv, const float* gate, void* grad_rows,
                float* dots, hipStream_t st) {
     const int P = s.n_tokens * s.top_k;
-    return by_size(s.n_tokens, s.top_k, [&](auto waves, auto kk) {
+    return by_size(s.d_model, s.top_k, [&](auto waves, auto kk) {
         constexpr int W = decltype(waves)::value, K = decltype(kk)::value;
-        const int grid = W == 1 ? (s.n_tokens + 3) / 4 : s.n_tokens;
+        const int grid = (s.n_tokens + 4 / W - 1) / (4 / W);
         const size_t lds = K == 0 && dots ? sizeof(float) * 4 * kWave * s.top_k : 0;
         const auto kern = !grad_rows ? spread_kernel<T, W, K, true, false> : dots ? spread_kernel<T, W, K, true, true> : spread_kernel<T, W, K, false, true>;
         static std::atomic<uint64_t> lds_allowed[2];
