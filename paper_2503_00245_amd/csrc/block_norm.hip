@@ -2,7 +2,9 @@
 // rows, and the gradient of both in one pass and a small sum over tokens (moe_training.h states them).
 //
 // A row is held in registers, so that every tensor is read once and written once: what bounds both is memory.
-// WAVES of a workgroup share a row of up to WAVES * 512 * CHUNKS values.
+// WAVES of a workgroup share a row of up to WAVES * 512 * CHUNKS values: eight values a lane (CHUNKS 1) leave the registers for the weights and the next
+// row.  (With a wave a row of 2048, 32 values a lane, weights read again for every row: 60 us forward, 131 back.)
+// 16384 rows of 2048, bf16, dropout: forward 55 us (268 MB, 4.9 TB/s), back 85 + 5 (403 MB and 19 MB of sums); 2048 rows of 1440 back 15.3 + 4.6.
 #include <algorithm>
 #include <cmath>
 
