@@ -380,7 +380,7 @@ RowPlan row_plan(int d) {
 int row_groups(int T, int d) { return row_plan(d).waves == 1 ? (T + 3) / 4 : T; }  // workgroups that have a row at all
 // Most workgroups of a pass.  Forward: 16384 rows of 2048, dropout, 1024 / 2048 / 4096 / 16384 of them 58.7 / 62.0 / 55.1 / 57.3 us.  Backward, four
 // waves of 132 registers each: 256 / 512 / 768 / 1024 of them 151 / 95.5 / 86 / 91 us; as many waves of other widths.
-constexpr int kGroups = 4096, kGradWaves = 3072;
+constexpr int kGroups = 4096, kGradWaves = 12 * 256;
 int most_grad_groups(int d) { return kGradWaves / std::max(row_plan(d).waves, row_plan(d).waves == 1 ? 4 : 1); }
 int grad_groups(int T, int d) { return std::min(most_grad_groups(d), row_groups(T, d)); }
 
