@@ -91,6 +91,23 @@ __global__ __launch_bounds__(kThreads) void dispatch_kernel(ptr_arg a_keys, ptr_
             atomicAdd(&s_all[e], all);
             atomicAdd(&s_run[e], before);
         }
+    } else if (E <= 4) {
+        // Few experts: lane e counts expert e by ballots.  LDS additions of a wave to one address come one after the other (8192 pairs, us, with them / by
+        // ballots: one expert 28.5 / 9.1, two 18.3 / 10.6, eight 15.2 / 23.3).
+        int all = 0, before = 0;
+        for (int q = wave * kWave; q < P; q += kThreads) {
+            const int key = live_key(keys, q + lane, P, E);
+            const unsigned long long early = q + kWave <= p0 ? ~0ull : q >= p0 ? 0ull : (1ull << (p0 - q)) - 1ull;
+            for (int e = 0; e < E; ++e) {
+                const unsigned long long is = __ballot(key == e);
+                all += lane == e ? __popcll(is) : 0;
+                before += lane == e ? __popcll(is & early) : 0;
+            }
+        }
+        if (lane < E) {
+            atomicAdd(&s_all[lane], all);
+            atomicAdd(&s_run[lane], before);
+        }
     } else {
         for (int p = threadIdx.x; p < P; p += kThreads) {
             const int e = live_key(keys, p, P, E);

@@ -245,7 +245,7 @@ extern "C" int moe_expert_ffn_backward(const moe_shape* shape, const moe_weights
     if (g.P == 0) return any_w ? run_grad_plain(g, GRAD_WEIGHTS, s.act_dtype, st) : MOE_OK;
     if (!weights || !x_perm || !grad_y_perm || !expert_offsets) return MOE_ERR_INVALID;
     for (const void* p : {weights->w_gate, weights->w_up, weights->w_down})
-        if (!p) return MOE_ERR_INVALID;
+        if (!p || p == grad_w_gate || p == grad_w_up || p == grad_w_down) return MOE_ERR_INVALID;  // (gradients do not take the weights' place: those are read after them)
     for (const void* p : {weights->w_gate, weights->w_up, weights->w_down, x_perm, grad_y_perm})
         if (!aligned16(p)) return MOE_ERR_INVALID;
     if (reinterpret_cast<uintptr_t>(expert_offsets) & 3u) return MOE_ERR_INVALID;

@@ -111,6 +111,8 @@ def test_gradient_of_experts_refuses():
     for n in ("w_gate", "w_up", "w_down"):
         assert call(fn, EXPERTS, w=_weights(**{n: 0})) == INVALID
         assert call(fn, EXPERTS, w=_weights(**{n: 4104})) == INVALID
+        for out in ("gg", "gu", "gd"):
+            assert call(fn, EXPERTS, w=_weights(**{n: EXPERTS[out].value})) == INVALID
     for n in ("gx", "gg", "gu", "gd"):
         assert call(fn, EXPERTS, **{n: P[0]}) == INVALID
         assert call(fn, EXPERTS, **{n: P[2]}) == INVALID
