@@ -2,6 +2,7 @@
 with bounds from the roundings on the way; the stack of such blocks; a training step of one, end to end and in a graph."""
 import importlib.util
 import os
+import threading
 
 import pytest
 import torch
@@ -294,11 +295,12 @@ def test_training_step_of_a_block(dtype, dropout, masked):
         assert rel(grads[n], w) < limit, n
 
 
-def test_training_steps_in_graphs_replay_what_the_eager_step_does():
+@pytest.mark.parametrize("T,d,F", [(48, 64, 136), (300, 264, 1032), (2500, 200, 264)])
+def test_training_steps_in_graphs_replay_what_the_eager_step_does(T, d, F):
     ex = _example()
-    layer = ex.Block(48, 64, 136, 8, 2, torch.bfloat16, 0.1, seed=4)
+    layer = ex.Block(T, d, F, 8, 2, torch.bfloat16, 0.1, seed=4)
     g = gen(9)
-    x, gy, pad = on(rnd(g, 48, 64, dtype=torch.bfloat16)), on(rnd(g, 48, 64, dtype=torch.bfloat16)), on(torch.zeros(48, dtype=torch.bool))
+    x, gy, pad = on(rnd(g, T, d, dtype=torch.bfloat16)), on(rnd(g, T, d, dtype=torch.bfloat16)), on(torch.rand(T, generator=g) < 0.1)
     side = torch.cuda.Stream()
     with torch.cuda.stream(side):
         layer.step(x, gy, pad)
@@ -308,7 +310,8 @@ def test_training_steps_in_graphs_replay_what_the_eager_step_does():
         with torch.cuda.graph(graph):
             outs.append(layer.step(x, gy, pad))
     for i in range(3):
-        x.copy_(rnd(g, 48, 64, dtype=torch.bfloat16))
+        x.copy_(rnd(g, T, d, dtype=torch.bfloat16))
+        layer.rng[1] += 1
         for graph, (y, grads, _) in zip(graphs, outs):
             graph.replay()
             torch.cuda.synchronize()
@@ -316,6 +319,36 @@ def test_training_steps_in_graphs_replay_what_the_eager_step_does():
             torch.cuda.synchronize()
             assert torch.equal(y, y2)
             assert all(torch.equal(grads[n], grads2[n]) for n in grads)
+
+
+def test_steps_of_two_threads_do_not_meet():
+    # each with a layer, a stream and workspaces of its own; what they compute alone is what they compute at once
+    ex = _example()
+    sizes = [(700, 264, 1032), (90, 520, 264)]
+    layers = [ex.Block(T, d, F, 8, 2, torch.bfloat16, 0.1, seed=i) for i, (T, d, F) in enumerate(sizes)]
+    data = [(on(rnd(gen(i), T, d, dtype=torch.bfloat16)), on(rnd(gen(i + 5), T, d, dtype=torch.bfloat16)), on(torch.zeros(T, dtype=torch.bool)))
+            for i, (T, d, F) in enumerate(sizes)]
+    alone = [layer.step(*args) for layer, args in zip(layers, data)]
+    torch.cuda.synchronize()
+    got, failed = [None, None], []
+
+    def work(i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(10):
+                    got[i] = layers[i].step(*data[i])
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:  # (a thread's own exception would go unseen)
+            failed.append(e)
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed
+    for (y, grads, idx), (y1, grads1, idx1) in zip(got, alone):
+        assert torch.equal(y, y1) and torch.equal(idx, idx1)
+        assert all(torch.equal(grads[n], grads1[n]) for n in grads)
 
 
 def test_calls_on_two_streams_do_not_meet():
