@@ -2,7 +2,7 @@
 // rows, and the gradient of both in one pass and a small sum over tokens (moe_training.h states them).
 //
 // A row is held in registers, so that every tensor is read once and written once: what bounds both is memory.
-// WAVES of a workgroup share a row of up to WAVES * 512 * CHUNKS values: eight values a lane (CHUNKS 1) leave the registers for the weights and the next
+// WAVES of a workgroup share a row of up to WAVES * 512 * CHUNKS values: eight values a lane (CHUNKS 1), or sixteen, leave the registers for the weights and the next
 // row.  (With a wave a row of 2048, 32 values a lane, weights read again for every row: 60 us forward, 131 back.)
 // 16384 rows of 2048, bf16, dropout: forward 55 us (268 MB, 4.9 TB/s), back 85 + 5 (403 MB and 19 MB of sums); 2048 rows of 1440 back 15.3 + 4.6.
 #include <algorithm>
@@ -113,12 +113,12 @@ struct RowPart {
     }
 };
 
-// Both kernels: workgroups take rows in turn.  What a lane needs of the [d] weights stays in its registers (up to 8192 values a row: eight
-// a lane), and the next row is on its way while one is summed.
+// Both kernels: workgroups take rows in turn.  What a lane needs of the [d] weights stays in its registers (up to 4096 values a row:
+// eight a lane; bf16 up to 8192: sixteen), and the next row is on its way while one is summed.
 template <typename T, int WAVES, int CHUNKS>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void block_norm_kernel(const BlockArgs g) {
     constexpr int ROWS = WAVES == 1 ? 4 : 1, STEP = WAVES * kWave * 8;
-    constexpr bool HOLD = CHUNKS == 1;
+    constexpr bool HOLD = CHUNKS == 1 || (WAVES == 8 && sizeof(T) == 2);
     __shared__ float s_sum[2 * 4 * WAVES];
     int turn = 0;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
@@ -206,7 +206,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void block_norm_k
 template <typename T, int WAVES, int CHUNKS, bool PARTS>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void block_grad_kernel(const BlockArgs g) {
     constexpr int ROWS = WAVES == 1 ? 4 : 1, STEP = WAVES * kWave * 8;
-    constexpr bool HOLD = CHUNKS == 1;
+    constexpr bool HOLD = CHUNKS == 1 || (WAVES == 8 && sizeof(T) == 2);
     __shared__ float s_sum[2 * 4 * WAVES];
     __shared__ float s_parts[PARTS && ROWS > 1 ? ROWS * kWave * 8 : 1];
     int turn = 0;
@@ -369,19 +369,26 @@ __global__ __launch_bounds__(1024) void block_parts_kernel(const float* __restri
     }
 }
 
-// Waves that share a row, chunks of 512 values that one of them holds
+// Waves that share a row, chunks of 512 values that one of them holds.  Rows of more than 4096 values: eight waves with two chunks have twice the registers
+// of sixteen with one (us, 16 x 1 / 8 x 2, 16384 rows of 8192: bf16 forward 276 / 225, back 395 / 374, fp32 back 1291 / 697; 3000 of 5120 45 / 34 and 60 / 61).
+// Two chunks of fp32 are too many to keep beside the next row's (back 882 so).
 struct RowPlan {
     int waves, chunks;
 };
 RowPlan row_plan(int d) {
     const int chunks = (d + 511) / 512;
-    return chunks <= 4 ? RowPlan{chunks, 1} : chunks <= 8 ? RowPlan{8, 1} : RowPlan{16, (chunks + 15) / 16};
+    return chunks <= 4 ? RowPlan{chunks, 1} : chunks <= 16 ? RowPlan{8, (chunks + 7) / 8} : RowPlan{16, (chunks + 15) / 16};
 }
 int row_groups(int T, int d) { return row_plan(d).waves == 1 ? (T + 3) / 4 : T; }  // workgroups that have a row at all
 // Most workgroups of a pass.  Forward: 16384 rows of 2048, dropout, 1024 / 2048 / 4096 / 16384 of them 58.7 / 62.0 / 55.1 / 57.3 us.  Backward, four
-// waves of 132 registers each: 256 / 512 / 768 / 1024 of them 151 / 95.5 / 86 / 91 us; as many waves of other widths.
+// waves of 132 registers each: 256 / 512 / 768 / 1024 of them 151 / 95.5 / 86 / 91 us; as many waves of narrower rows.  Of eight waves and more a CU holds one
+// workgroup: 256 of them (4096 rows of 4096 384 / 256 of them 72 / 58 us; 1024 of 16384, 16 waves, 192 / 256 124 / 112, 512 of
+// 32768 254 / 282 in bf16 and 445 / 406 in fp32).
 constexpr int kGroups = 4096, kGradWaves = 12 * 256;
-int most_grad_groups(int d) { return kGradWaves / std::max(row_plan(d).waves, row_plan(d).waves == 1 ? 4 : 1); }
+int most_grad_groups(int d) {
+    const int waves = row_plan(d).waves;
+    return waves > 4 ? 256 : kGradWaves / (waves == 1 ? 4 : waves);
+}
 int grad_groups(int T, int d) { return std::min(most_grad_groups(d), row_groups(T, d)); }
 
 template <typename F>
@@ -397,8 +404,8 @@ int by_plan(RowPlan p, F run) {
         case 2: return run(c2{}, c1{});
         case 3: return run(c3{}, c1{});
         case 4: return run(c4{}, c1{});
-        case 8: return run(c8{}, c1{});
-        default: return p.chunks == 1 ? run(c16{}, c1{}) : p.chunks == 2 ? run(c16{}, c2{}) : p.chunks == 3 ? run(c16{}, c3{}) : run(c16{}, c4{});
+        case 8: return p.chunks == 1 ? run(c8{}, c1{}) : run(c8{}, c2{});
+        default: return p.chunks == 2 ? run(c16{}, c2{}) : p.chunks == 3 ? run(c16{}, c3{}) : run(c16{}, c4{});
     }
 }
 

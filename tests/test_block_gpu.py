@@ -32,7 +32,7 @@ def block_of(cfg):
     return pkg.make_block(**{n: on(v) if torch.is_tensor(v) else v for n, v in cfg.items()})
 
 
-SHAPES = [(1, 8), (1, 2048), (3, 40), (17, 512), (5, 520), (130, 432), (2049, 1440), (2500, 64), (3, 8192), (2, 8200), (1, 32768), (600, 2056), (210, 8200)]
+SHAPES = [(1, 8), (1, 2048), (3, 40), (17, 512), (5, 520), (130, 432), (2049, 1440), (2500, 64), (3, 8192), (2, 8200), (1, 32768), (600, 2056), (210, 8200), (520, 5000), (300, 8192)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -90,7 +90,7 @@ def test_block(T, d, what, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("T,d", [(17001, 40), (4501, 520), (9001, 1032), (4500, 2056), (4200, 4104), (4105, 8200)])
+@pytest.mark.parametrize("T,d", [(17001, 40), (4501, 520), (9001, 1032), (4500, 2056), (4200, 4104), (4105, 8200), (4300, 6152)])
 def test_rows_do_not_depend_on_the_rows_around_them(T, d, dtype):
     # workgroups that take many rows in turn give every row what a call of a few rows gives it, bit for bit
     dt = DTYPES[dtype]
