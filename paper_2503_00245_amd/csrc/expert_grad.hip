@@ -4,9 +4,9 @@
 // The forward pass keeps nothing for it: a and b are formed again (4 of 16 P d F operations), which is less than what reading
 // them back would save in any program that holds more than a few layers' worth of rows.
 //
-// The kernels here: tiles of 64 x 64 on four waves, operands widened to fp32 in LDS, v_mfma_f32_16x16x4_f32, a layout of operands that the k axis of
-// either kind of product needs no transposition for.  97 to 108 TFLOP/s from 2048 tokens of 2048 / 5632 on (the fp32 matrix rate is 157); they
-// serve fp32 layers, which are the small ones, and layers too narrow for expert_grad_mfma.hip.
+// The kernels here: tiles of 64 x 64, or 32 x 32 where those are few, on four waves, operands widened to fp32 in LDS, v_mfma_f32_16x16x4_f32, a layout of
+// operands that the k axis of either kind of product needs no transposition for.  97 to 108 TFLOP/s from 2048 tokens of 2048 / 5632 on (the fp32 matrix rate
+// is 157); they serve fp32 layers, which are the small ones, and layers too narrow for expert_grad_mfma.hip.
 #include "expert_grad.h"
 #include "expert_grad_plan.h"
 
@@ -15,26 +15,37 @@ namespace moe {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int TILE = 64, STEP = 16, PITCH = TILE + 4;
+// Tiles of 64 by 64 up to which 32 by 32 ones are taken: a tile's k-steps follow one another, and smaller ones put more CUs to work on them.  (us, 64 / 32 by
+// these: fp32, 10 tokens of 384 / 512, 4 of 4 experts, 73 / 38, 168 of 144 / 880 82 / 50, 300 of 256 / 512 79 / 49; bf16, 2048 of 128 / 1152 287 / 202.
+// Beyond: the rows' gradient of 2048 of 432 / 1152, 504 tiles, 13 us longer in small ones)
+constexpr int kFewRowTiles = 256, kFewWeightTiles = 1024;
 
-// A tile's share of one operand: 16 k by 64 rows (or columns) in fp32, [k][row].  K_CONTIGUOUS: memory holds [row][k].
-template <typename T, bool K_CONTIGUOUS>
+// Tiles of SIDE by SIDE on four waves, k-steps of STEP, AHEAD of which are on their way while one is multiplied
+template <int SIDE_>
+struct Form {
+    static constexpr int SIDE = SIDE_, STEP = 4 * kThreads / SIDE, PITCH = SIDE + 4, AHEAD = SIDE == 32 ? 4 : 2, NB = SIDE / 32;
+    float a[2][STEP][PITCH], b[2][STEP][PITCH];
+};
+
+// A tile's share of one operand: STEP k by SIDE rows (or columns) in fp32, [k][row].  K_CONTIGUOUS: memory holds [row][k].
+template <typename F, typename T, bool K_CONTIGUOUS>
 struct Operand {
+    static constexpr int PER_ROW = K_CONTIGUOUS ? F::STEP / 4 : F::SIDE / 4;  // threads that share a row of memory
     const T* base;       // of the expert's matrix or the group's first row
     long long pitch;     // elements from one row of memory to the next
     int rows, K;         // valid rows (columns) from `first` on, valid k
     int first;
 
     __device__ __forceinline__ f32x4 load(int k0) const {
-        const int t = threadIdx.x;
+        const int t = threadIdx.x, along = t % PER_ROW * 4, across = t / PER_ROW;
         const T* p;
         bool ok;
         if (K_CONTIGUOUS) {  // four k of a row
-            const int r = t >> 2, k = k0 + (t & 3) * 4;
+            const int r = across, k = k0 + along;
             ok = r < rows && k < K;
             p = base + (first + r) * pitch + k;
         } else {             // four rows of a k
-            const int r = (t & 15) * 4, k = k0 + (t >> 4);
+            const int r = along, k = k0 + across;
             ok = r < rows && k < K;
             p = base + k * pitch + first + r;
         }
@@ -50,42 +61,48 @@ struct Operand {
         }
         return v;
     }
-    __device__ __forceinline__ void store(float (*s)[PITCH], const f32x4& v) const {
-        const int t = threadIdx.x;
+    __device__ __forceinline__ void store(float (*s)[F::PITCH], const f32x4& v) const {
+        const int t = threadIdx.x, along = t % PER_ROW * 4, across = t / PER_ROW;
         if (K_CONTIGUOUS) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[(t & 3) * 4 + i][t >> 2] = v[i];
+            for (int i = 0; i < 4; ++i) s[along + i][across] = v[i];
         } else {
-            *reinterpret_cast<f32x4*>(&s[t >> 4][(t & 15) * 4]) = v;
+            *reinterpret_cast<f32x4*>(&s[across][along]) = v;
         }
     }
 };
 
-struct Tile {
-    float a[STEP][PITCH], b[STEP][PITCH];
-};
-
-// acc[i][j] += the products of 16-row block i and 16-column block j of the wave's 32 x 32; a lane's four values are neighbouring
+// acc[i][j] += the products of 16-row block i and 16-column block j of the wave's quarter; a lane's four values are neighbouring
 // columns of one row
-template <typename OA, typename OB>
-__device__ __forceinline__ void multiply(Tile& s, const OA& a, const OB& b, int K, f32x4 (&acc)[2][2]) {
+template <typename F, typename OA, typename OB>
+__device__ __forceinline__ void multiply(F& s, const OA& a, const OB& b, int K, f32x4 (&acc)[F::NB][F::NB]) {
+    constexpr int STEP = F::STEP, AHEAD = F::AHEAD, NB = F::NB;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const int m0 = (wave >> 1) * 32 + (lane & 15), n0 = (wave & 1) * 32 + (lane & 15);
-    f32x4 va = a.load(0), vb = b.load(0);
-    for (int k0 = 0; k0 < K; k0 += STEP) {
-        __syncthreads();
-        a.store(s.a, va);
-        b.store(s.b, vb);
-        __syncthreads();
-        if (k0 + STEP < K) va = a.load(k0 + STEP), vb = b.load(k0 + STEP);
+    const int m0 = (wave >> 1) * (F::SIDE / 2) + (lane & 15), n0 = (wave & 1) * (F::SIDE / 2) + (lane & 15);
+    f32x4 va[AHEAD], vb[AHEAD];
 #pragma unroll
-        for (int k = 0; k < STEP; k += 4) {
-            const int kk = k + (lane >> 4);
-            const float a0 = s.a[kk][m0], a1 = s.a[kk][m0 + 16], b0 = s.b[kk][n0], b1 = s.b[kk][n0 + 16];
-            acc[0][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(b0, a0, acc[0][0], 0, 0, 0);
-            acc[0][1] = __builtin_amdgcn_mfma_f32_16x16x4f32(b1, a0, acc[0][1], 0, 0, 0);
-            acc[1][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(b0, a1, acc[1][0], 0, 0, 0);
-            acc[1][1] = __builtin_amdgcn_mfma_f32_16x16x4f32(b1, a1, acc[1][1], 0, 0, 0);
+    for (int j = 0; j < AHEAD; ++j) va[j] = a.load(j * STEP), vb[j] = b.load(j * STEP);
+    __syncthreads();  // (what was multiplied before has been read)
+    for (int k0 = 0; k0 < K; k0 += AHEAD * STEP) {
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            if (k0 + j * STEP >= K) break;
+            float(*const sa)[F::PITCH] = s.a[j & 1], (*const sb)[F::PITCH] = s.b[j & 1];
+            a.store(sa, va[j]);
+            b.store(sb, vb[j]);
+            __syncthreads();
+            va[j] = a.load(k0 + (j + AHEAD) * STEP), vb[j] = b.load(k0 + (j + AHEAD) * STEP);
+#pragma unroll
+            for (int k = 0; k < STEP; k += 4) {
+                const int kk = k + (lane >> 4);
+                float fa[NB], fb[NB];
+#pragma unroll
+                for (int i = 0; i < NB; ++i) fa[i] = sa[kk][m0 + 16 * i], fb[i] = sb[kk][n0 + 16 * i];
+#pragma unroll
+                for (int i = 0; i < NB; ++i)
+#pragma unroll
+                    for (int q = 0; q < NB; ++q) acc[i][q] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[q], fa[i], acc[i][q], 0, 0, 0);
+            }
         }
     }
 }
@@ -96,9 +113,10 @@ __device__ __forceinline__ void put4(T* p, const f32x4& v) {
     for (int i = 0; i < 4; ++i) p[i] = Store<T>::from_f32(v[i]);
 }
 
-template <typename T, int OP>
+template <typename F, typename T, int OP>
 __global__ __launch_bounds__(kThreads) void grad_rows_kernel(const GradArgs g) {
-    __shared__ Tile s;
+    constexpr int TILE = F::SIDE, NB = F::NB;
+    __shared__ F s;
     const int K = OP == GRAD_DX ? g.F : g.d, N = OP == GRAD_DX ? g.d : g.F;
     int lo, hi, e, row0, row_end, nt;
     group_bounds(g.offsets, g.E, g.P, lo, hi);
@@ -107,27 +125,27 @@ __global__ __launch_bounds__(kThreads) void grad_rows_kernel(const GradArgs g) {
     const int n0 = nt * TILE;
     const size_t at_w = (size_t)e * g.d * g.F;
     const int rows = min(TILE, row_end - row0), cols = min(TILE, N - n0);
-    f32x4 acc[2][2] = {}, up[2][2] = {}, dh[2][2] = {};
+    f32x4 acc[NB][NB] = {}, up[NB][NB] = {}, dh[NB][NB] = {};
     if (OP == GRAD_ACT) {
-        const Operand<T, true> a{static_cast<const T*>(g.x), g.d, rows, K, row0};
-        const Operand<T, true> b{static_cast<const T*>(g.w_gate) + at_w, g.d, cols, K, n0}, b1{static_cast<const T*>(g.w_up) + at_w, g.d, cols, K, n0};
+        const Operand<F, T, true> a{static_cast<const T*>(g.x), g.d, rows, K, row0};
+        const Operand<F, T, true> b{static_cast<const T*>(g.w_gate) + at_w, g.d, cols, K, n0}, b1{static_cast<const T*>(g.w_up) + at_w, g.d, cols, K, n0};
         multiply(s, a, b, K, acc);
         multiply(s, a, b1, K, up);
-        const Operand<T, true> a2{static_cast<const T*>(g.gy), g.d, rows, K, row0};
-        const Operand<T, false> b2{static_cast<const T*>(g.w_down) + at_w, g.F, cols, K, n0};
+        const Operand<F, T, true> a2{static_cast<const T*>(g.gy), g.d, rows, K, row0};
+        const Operand<F, T, false> b2{static_cast<const T*>(g.w_down) + at_w, g.F, cols, K, n0};
         multiply(s, a2, b2, K, dh);
     } else {
-        const Operand<T, true> a{static_cast<const T*>(g.da), g.F, rows, K, row0}, a1{static_cast<const T*>(g.db), g.F, rows, K, row0};
-        const Operand<T, false> b{static_cast<const T*>(g.w_gate) + at_w, g.d, cols, K, n0}, b1{static_cast<const T*>(g.w_up) + at_w, g.d, cols, K, n0};
+        const Operand<F, T, true> a{static_cast<const T*>(g.da), g.F, rows, K, row0}, a1{static_cast<const T*>(g.db), g.F, rows, K, row0};
+        const Operand<F, T, false> b{static_cast<const T*>(g.w_gate) + at_w, g.d, cols, K, n0}, b1{static_cast<const T*>(g.w_up) + at_w, g.d, cols, K, n0};
         multiply(s, a, b, K, acc);
         multiply(s, a1, b1, K, acc);
     }
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < NB; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int r = (wave >> 1) * 32 + i * 16 + (lane & 15), c = (wave & 1) * 32 + j * 16 + (lane >> 4) * 4;
+        for (int j = 0; j < NB; ++j) {
+            const int r = (wave >> 1) * (TILE / 2) + i * 16 + (lane & 15), c = (wave & 1) * (TILE / 2) + j * 16 + (lane >> 4) * 4;
             if (r >= rows || c >= cols) continue;
             const size_t at = (size_t)(row0 + r) * N + n0 + c;
             if (OP == GRAD_ACT) {
@@ -147,9 +165,10 @@ __global__ __launch_bounds__(kThreads) void grad_rows_kernel(const GradArgs g) {
 }
 
 // blockIdx.y: expert, z: which of the three gradients
-template <typename T>
+template <typename F, typename T>
 __global__ __launch_bounds__(kThreads) void grad_weights_kernel(const GradArgs g) {
-    __shared__ Tile s;
+    constexpr int TILE = F::SIDE, NB = F::NB;
+    __shared__ F s;
     const int e = blockIdx.y, which = blockIdx.z;
     const int M = which == 2 ? g.d : g.F, N = which == 2 ? g.F : g.d;
     T* const out = static_cast<T*>(which == 0 ? g.gw_gate : which == 1 ? g.gw_up : g.gw_down);
@@ -159,35 +178,42 @@ __global__ __launch_bounds__(kThreads) void grad_weights_kernel(const GradArgs g
     if (n0 >= N) return;
     const int lo = g.P ? min(max(g.offsets[e], 0), g.P) : 0, hi = g.P ? min(max(g.offsets[e + 1], lo), g.P) : 0;
     const int rows = min(TILE, M - m0), cols = min(TILE, N - n0), K = hi - lo;
-    f32x4 acc[2][2] = {};
+    f32x4 acc[NB][NB] = {};
     if (K > 0) {
         const T* const left = static_cast<const T*>(which == 0 ? g.da : which == 1 ? g.db : g.gy) + (size_t)lo * M;
         const T* const right = static_cast<const T*>(which == 2 ? g.h : g.x) + (size_t)lo * N;
-        const Operand<T, false> a{left, M, rows, K, m0}, b{right, N, cols, K, n0};
+        const Operand<F, T, false> a{left, M, rows, K, m0}, b{right, N, cols, K, n0};
         multiply(s, a, b, K, acc);
     }
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < NB; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int r = (wave >> 1) * 32 + i * 16 + (lane & 15), c = (wave & 1) * 32 + j * 16 + (lane >> 4) * 4;
+        for (int j = 0; j < NB; ++j) {
+            const int r = (wave >> 1) * (TILE / 2) + i * 16 + (lane & 15), c = (wave & 1) * (TILE / 2) + j * 16 + (lane >> 4) * 4;
             if (r < rows && c < cols) put4(out + (size_t)e * M * N + (size_t)(m0 + r) * N + n0 + c, acc[i][j]);
         }
 }
 
-template <typename T>
-int run_plain(const GradArgs& g, GradOp op, hipStream_t st) {
+template <typename F, typename T>
+int run_tiles(const GradArgs& g, GradOp op, hipStream_t st) {
+    constexpr int TILE = F::SIDE;
     if (op == GRAD_WEIGHTS) {
         const unsigned tiles = (unsigned)((g.d + TILE - 1) / TILE) * ((g.F + TILE - 1) / TILE);
-        hipLaunchKernelGGL(grad_weights_kernel<T>, dim3(tiles, g.E, 3), dim3(kThreads), 0, st, g);
+        hipLaunchKernelGGL((grad_weights_kernel<F, T>), dim3(tiles, g.E, 3), dim3(kThreads), 0, st, g);
         return launch_status();
     }
     const int N = op == GRAD_DX ? g.d : g.F;
     const int grid = find_tile_grid(m_tiles_bound(g.P, g.E, TILE) * ((N + TILE - 1) / TILE), 0);
-    const auto kern = op == GRAD_ACT ? grad_rows_kernel<T, GRAD_ACT> : grad_rows_kernel<T, GRAD_DX>;
+    const auto kern = op == GRAD_ACT ? grad_rows_kernel<F, T, GRAD_ACT> : grad_rows_kernel<F, T, GRAD_DX>;
     hipLaunchKernelGGL(kern, dim3(grid), dim3(kThreads), 0, st, g);
     return launch_status();
+}
+template <typename T>
+int run_plain(const GradArgs& g, GradOp op, hipStream_t st) {
+    const int N = op == GRAD_DX ? g.d : g.F;
+    const long long tiles = op == GRAD_WEIGHTS ? 3ll * g.E * ((g.d + 63) / 64) * ((g.F + 63) / 64) : (long long)m_tiles_bound(g.P, g.E, 64) * ((N + 63) / 64);
+    return tiles <= (op == GRAD_WEIGHTS ? kFewWeightTiles : kFewRowTiles) ? run_tiles<Form<32>, T>(g, op, st) : run_tiles<Form<64>, T>(g, op, st);
 }
 
 struct GradLayout {
@@ -203,8 +229,8 @@ int validate_grad(const moe_shape* s) {
     const int rc = validate_shape(s);
     if (rc != MOE_OK) return rc;
     // a launch has fewer than 2^32 threads: tiles of 64 by 64 of the rows' products, strips of 256 hidden columns by tiles across d of the weights'
-    const long long tiles_d = (s->d_model + TILE - 1) / TILE, tiles_f = (s->d_ff + TILE - 1) / TILE;
-    const long long rows = ((long long)s->n_tokens * s->top_k + TILE - 1) / TILE + s->n_experts;
+    const long long tiles_d = (s->d_model + 63) / 64, tiles_f = (s->d_ff + 63) / 64;
+    const long long rows = ((long long)s->n_tokens * s->top_k + 63) / 64 + s->n_experts;
     if (s->rank != 0 || s->d_model > (1 << 18) || s->d_ff > (1 << 18) || tiles_d * tiles_f >= (1 << 23) || rows * (tiles_d > tiles_f ? tiles_d : tiles_f) >= (1 << 23) ||
         (s->n_experts * 3ll * ((s->d_ff + 255) / 256) + 8) * 2 * ((s->d_model + 255) / 256) >= (1 << 23))
         return MOE_ERR_UNSUPPORTED;
