@@ -27,8 +27,11 @@ extern "C" {
  * Of the shape d_model, n_tokens, n_experts, top_k and act_dtype are read (d_ff has to be valid).
  */
 
-/* Bytes of workspace that moe_dispatch and moe_expert_ffn_backward need for this shape (0 if invalid, or of rank > 0).  Does not
- * fall as n_tokens grows. */
+/* Bytes of workspace that moe_dispatch needs for this shape, whatever its experts (0 if invalid).  Does not fall as n_tokens grows. */
+MOE_API size_t moe_dispatch_workspace_bytes(const moe_shape* shape);
+
+/* Bytes of workspace that moe_expert_ffn_backward needs for this shape, and as many as moe_dispatch needs; 0 if moe_expert_ffn_backward
+ * refuses the shape (see there).  As far as it takes them, does not fall as n_tokens grows. */
 MOE_API size_t moe_training_workspace_bytes(const moe_shape* shape);
 
 /*
@@ -39,7 +42,7 @@ MOE_API size_t moe_training_workspace_bytes(const moe_shape* shape);
  *   perm           [P]    int32 out: the pair of each row, -1 from offsets[E] on
  *   inv_perm       [P]    int32 out: the row of each pair, -1 if it is switched off
  *   x_perm         [P, d] act_dtype out: x_perm[s] = weight[perm[s]] x[perm[s] / k]; zeros from offsets[E] on
- * The workspace is 4-byte aligned.
+ * workspace: moe_dispatch_workspace_bytes(shape), 4-byte aligned; up to 8192 pairs it is not needed (NULL will do).
  */
 MOE_API int moe_dispatch(const moe_shape* shape, const int32_t* topk_idx, const float* weight, const void* x,
                          int32_t* expert_offsets, int32_t* perm, int32_t* inv_perm, void* x_perm,
@@ -85,6 +88,8 @@ MOE_API int moe_collect_backward(const moe_shape* shape, const void* grad_y, con
  *   weights: w_gate, w_up [E, F, d], w_down [E, d, F] (the other fields are not read)
  *   grad_x_perm [P, d]; grad_w_gate, grad_w_up [E, F, d], grad_w_down [E, d, F] act_dtype out, each of them or NULL
  * Of no tokens the gradients of weights are zero.  workspace: moe_training_workspace_bytes(shape), 16-byte aligned.
+ * Unsupported are rank > 0, d or F over 2^18, and layers of more tiles than a launch has: d' F', (ceil(P / 64) + E) max(d', F') and
+ * (3 E ceil(F / 256) + 8) 2 ceil(d / 256) have to be below 2^23, with d' = ceil(d / 64), F' = ceil(F / 64).
  */
 MOE_API int moe_expert_ffn_backward(const moe_shape* shape, const moe_weights* weights, const void* x_perm,
                                     const int32_t* expert_offsets, const void* grad_y_perm, void* grad_x_perm,

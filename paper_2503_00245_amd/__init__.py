@@ -9,7 +9,7 @@ from .binding import (  # noqa: F401
     QUANTISED_EXPORTS, Mxfp4Weights, RouteConfig, SCORE_SIGMOID, SCORE_SOFTMAX, alloc_mxfp4_workspace, make_mxfp4_weights, make_route_config,
     moe_mxfp4_dequantize, moe_mxfp4_experts, moe_mxfp4_forward, moe_mxfp4_pack, moe_mxfp4_quantize, moe_mxfp4_workspace_bytes,
     moe_route_scored, moe_route_scored_backward,
-    TRAINING_EXPORTS, Block, alloc_block_stack_workspace, alloc_block_workspace, alloc_training_workspace, make_block, moe_block_norm,
+    TRAINING_EXPORTS, Block, alloc_block_stack_workspace, alloc_block_workspace, alloc_dispatch_workspace, alloc_training_workspace, make_block, moe_block_norm,
     moe_block_norm_backward, moe_block_stack_forward, moe_block_stack_workspace_bytes, moe_block_workspace_bytes, moe_collect, moe_collect_backward,
-    moe_dispatch, moe_dispatch_backward, moe_expert_ffn_backward, moe_training_workspace_bytes,
+    moe_dispatch, moe_dispatch_backward, moe_dispatch_workspace_bytes, moe_expert_ffn_backward, moe_training_workspace_bytes,
 )

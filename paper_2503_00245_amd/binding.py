@@ -27,7 +27,7 @@ EXPORTS = ("moe_route", "moe_permute", "moe_expert_ffn", "moe_combine", "moe_for
 QUANTISED_EXPORTS = ("moe_route_scored", "moe_route_scored_backward", "moe_mxfp4_quantize", "moe_mxfp4_dequantize",
                      "moe_mxfp4_packed_bytes", "moe_mxfp4_pack", "moe_mxfp4_workspace_bytes", "moe_mxfp4_experts",
                      "moe_mxfp4_forward")  # include/moe_quantised.h
-TRAINING_EXPORTS = ("moe_training_workspace_bytes", "moe_dispatch", "moe_dispatch_backward", "moe_collect", "moe_collect_backward",
+TRAINING_EXPORTS = ("moe_dispatch_workspace_bytes", "moe_training_workspace_bytes", "moe_dispatch", "moe_dispatch_backward", "moe_collect", "moe_collect_backward",
                     "moe_expert_ffn_backward", "moe_block_norm", "moe_block_workspace_bytes", "moe_block_norm_backward",
                     "moe_block_stack_workspace_bytes", "moe_block_stack_forward")  # include/moe_training.h
 
@@ -111,10 +111,11 @@ def lib() -> C.CDLL:
         L.moe_mxfp4_experts.argtypes = [sp, qp, vp, vp, vp, vp, vp, sz, vp]
         L.moe_mxfp4_forward.argtypes = [sp, rp, qp, vp, vp, vp, vp, vp, vp, sz, vp]
         bp = C.POINTER(BlockStruct)
+        L.moe_dispatch_workspace_bytes.argtypes = [sp]
         L.moe_training_workspace_bytes.argtypes = [sp]
         L.moe_block_workspace_bytes.argtypes = [i32, i32]
         L.moe_block_stack_workspace_bytes.argtypes = [sp]
-        for fn in ("moe_training_workspace_bytes", "moe_block_workspace_bytes", "moe_block_stack_workspace_bytes"):
+        for fn in ("moe_dispatch_workspace_bytes", "moe_training_workspace_bytes", "moe_block_workspace_bytes", "moe_block_stack_workspace_bytes"):
             getattr(L, fn).restype = sz
         L.moe_dispatch.argtypes = [sp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.moe_dispatch_backward.argtypes = [sp, vp, vp, vp, vp, vp, vp, vp]
@@ -488,6 +489,18 @@ def moe_mxfp4_forward(shape: MoeShape, config: RouteConfig, weights: Mxfp4Weight
 
 
 # ---- a training step around and through the experts --------------------------------------------------------------
+
+def moe_dispatch_workspace_bytes(shape: MoeShape) -> int:
+    return int(lib().moe_dispatch_workspace_bytes(C.byref(shape)))
+
+
+def alloc_dispatch_workspace(shape: MoeShape, device) -> torch.Tensor:
+    """moe_dispatch's workspace, of any layer (alloc_training_workspace's serves it too, where the experts' gradient takes the layer)"""
+    n = moe_dispatch_workspace_bytes(shape)
+    if n == 0:
+        raise MoeError("moe_dispatch_workspace_bytes", -1)
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
 
 def moe_training_workspace_bytes(shape: MoeShape) -> int:
     return int(lib().moe_training_workspace_bytes(C.byref(shape)))

@@ -450,6 +450,10 @@ size_t dispatch_scratch_bytes(long long T, int E) {
 
 using namespace moe;
 
+extern "C" size_t moe_dispatch_workspace_bytes(const moe_shape* shape) {
+    return validate_shape(shape) == MOE_OK ? round_up(dispatch_scratch_bytes(shape->n_tokens, shape->n_experts), 256) : 0;
+}
+
 extern "C" int moe_dispatch(const moe_shape* shape, const int32_t* topk_idx, const float* weight, const void* x, int32_t* expert_offsets,
                             int32_t* perm, int32_t* inv_perm, void* x_perm, void* workspace, size_t workspace_bytes, void* stream) {
     int rc = validate_shape(shape);

@@ -1,0 +1,45 @@
+"""What a call around the experts needs is told for every shape that it accepts: sizes of workspaces, and which forms of the kernels the GPU tests reach."""
+import ctypes as C
+
+import pytest
+import torch
+
+import paper_2503_00245_amd as pkg
+
+WORKSPACE = -3
+P = [C.c_void_p(i << 20) for i in range(1, 9)]  # addresses that no launch will see
+
+
+def dispatch_on_the_host(shape, nbytes):
+    """moe_dispatch's answer where its workspace has nbytes, but is misaligned: it is refused after its size has been looked at"""
+    args = [C.byref(shape), P[0], None, P[1], P[2], P[3], P[4], P[5], C.c_void_p((7 << 20) + 2), nbytes, None]
+    return pkg.lib().moe_dispatch(*args)
+
+
+# weight-decomposed experts, experts with a shared base, experts wider than the gradient takes, more rows than it takes
+SHAPES = [dict(rank=64), dict(rank=64, flags=pkg.FLAG_SHARED_BASE), dict(d_ff=(1 << 18) + 8), dict(d_model=(1 << 18) + 8), dict(n_tokens=1 << 20, d_model=1024, d_ff=28672),
+          dict(n_tokens=(1 << 23) - 1), dict(n_experts=64, top_k=64), dict(n_experts=1, top_k=1, n_tokens=9000), dict(act_dtype=pkg.MOE_F32, rank=8)]
+
+
+@pytest.mark.parametrize("kw", SHAPES)
+def test_dispatch_tells_its_workspace_for_every_shape_it_takes(kw):
+    shape = pkg.make_shape(**dict(dict(n_tokens=5000, d_model=64, d_ff=136, n_experts=8, top_k=2), **kw))
+    need = pkg.moe_dispatch_workspace_bytes(shape)
+    assert need > 0
+    assert dispatch_on_the_host(shape, 4) == WORKSPACE
+    assert dispatch_on_the_host(shape, need) == -1  # large enough; refused for its alignment
+    assert pkg.alloc_dispatch_workspace(shape, "cpu").nbytes == need
+    gradient = pkg.moe_training_workspace_bytes(shape)
+    assert gradient == 0 or gradient >= need  # (where the gradient takes the shape, its workspace serves both)
+
+
+def test_sizes_of_dispatch_refuse_and_do_not_fall():
+    for kw in (dict(top_k=0), dict(n_tokens=-1), dict(d_model=60), dict(n_experts=65), dict(n_tokens=1 << 23), dict(flags=4)):
+        shape = pkg.make_shape(**dict(dict(n_tokens=8, d_model=64, d_ff=136, n_experts=4, top_k=2), **kw))
+        assert pkg.moe_dispatch_workspace_bytes(shape) == 0, kw
+        with pytest.raises(pkg.MoeError):
+            pkg.alloc_dispatch_workspace(shape, "cpu")
+    for E, k in ((1, 1), (3, 2), (8, 2), (60, 6), (64, 64)):
+        sizes = [pkg.moe_dispatch_workspace_bytes(pkg.make_shape(t, 64, 136, E, k, rank=64)) for t in [*range(3000), *range(3000, 200000, 97)]]
+        assert sizes[0] > 0 and all(a <= b for a, b in zip(sizes, sizes[1:]))
+    assert pkg.alloc_dispatch_workspace(pkg.make_shape(0, 64, 136, 4, 2), "cpu").dtype is torch.uint8
