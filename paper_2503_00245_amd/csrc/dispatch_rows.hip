@@ -8,6 +8,7 @@
 
 #include "moe_training.h"
 #include "rows8.h"
+#include "rows_plan.h"
 
 namespace moe {
 
@@ -15,21 +16,6 @@ namespace {
 
 constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / kWave;
-// Pairs up to which every workgroup counts all keys itself, and counting needs no launch of its own (us, so / with that launch: 96 pairs of 16 experts
-// 5.6 / 8.1, 2048 pairs of 8 6.8 / 8.8, 4096 of 8 10.0 / 10.7, of 64 8.2 / 11.8, 8192 of 64 11.6 / 14.0, of 8 15.2 / 13.9, 16384 of 8 20.2 / 14.3)
-constexpr int kKeysAlone = 8192;
-constexpr int kMaxCounts = 16384;  // counts that a workgroup adds up beyond
-
-// Chunks of whole tokens: about two workgroups a CU, no more chunks than their counts may be
-struct DispatchPlan {
-    int tokens;  // of a chunk
-    int chunks;
-};
-DispatchPlan dispatch_plan(long long T, int E) {
-    const long long most = std::min(512, kMaxCounts / E);
-    const long long tokens = std::max<long long>(4, (T + most - 1) / most);
-    return DispatchPlan{(int)tokens, (int)((T + tokens - 1) / tokens)};
-}
 
 __device__ __forceinline__ int live_key(const int32_t* keys, int p, int end, int E) {  // the pair's expert; E: it has none
     const int key = p < end ? keys[p] : E;
@@ -91,9 +77,7 @@ __global__ __launch_bounds__(kThreads) void dispatch_kernel(ptr_arg a_keys, ptr_
             atomicAdd(&s_all[e], all);
             atomicAdd(&s_run[e], before);
         }
-    } else if (E <= 4) {
-        // Few experts: lane e counts expert e by ballots.  LDS additions of a wave to one address come one after the other (8192 pairs, us, with them / by
-        // ballots: one expert 28.5 / 9.1, two 18.3 / 10.6, eight 15.2 / 23.3).
+    } else if (E <= kBallotExperts) {  // lane e counts expert e
         int all = 0, before = 0;
         for (int q = wave * kWave; q < P; q += kThreads) {
             const int key = live_key(keys, q + lane, P, E);
@@ -386,21 +370,23 @@ __global__ __launch_bounds__(256) void spread_kernel(ptr_arg a_inv, ptr_arg a_ga
 
 constexpr size_t kDotsLds = sizeof(float) * 4 * kWave * kMaxExperts;  // dot products of 64 pairs, a sum per lane
 
-// A wave for every 512 values, up to four (us, one wave / four / so: collect of 16384 tokens of 432, two experts, 7.8 / 9.6 / 7.8, 2048 of 2048 4.8 / 4.1 / 4.2;
-// its gradient at 16384 of 2048 68.0 / 65.0 / 62.8, 8192 of 1024 14.4 / 15.6 / 14.7, 2048 of 720, eight experts, 11.5 / 13.6 / 10.4)
 template <typename F>
 int by_size(int d, int k, F run) {
-    typedef std::integral_constant<int, 1> one;
-    typedef std::integral_constant<int, 2> two;
-    typedef std::integral_constant<int, 4> four;
+    const RowsForm form = rows_form(d, k);
     auto on = [&](auto waves) {
-        if (k == 1) return run(waves, one{});
-        if (k == 2) return run(waves, two{});
-        if (k <= 4) return run(waves, four{});
-        if (k <= 8) return run(waves, std::integral_constant<int, 8>{});
-        return run(waves, std::integral_constant<int, 0>{});
+        switch (form.pairs) {
+            case 1: return run(waves, std::integral_constant<int, 1>{});
+            case 2: return run(waves, std::integral_constant<int, 2>{});
+            case 4: return run(waves, std::integral_constant<int, 4>{});
+            case 8: return run(waves, std::integral_constant<int, 8>{});
+            default: return run(waves, std::integral_constant<int, 0>{});
+        }
     };
-    return d <= 512 ? on(one{}) : d <= 1024 ? on(two{}) : on(four{});
+    switch (form.waves) {
+        case 1: return on(std::integral_constant<int, 1>{});
+        case 2: return on(std::integral_constant<int, 2>{});
+        default: return on(std::integral_constant<int, 4>{});
+    }
 }
 
 template <typename T>
@@ -468,7 +454,7 @@ extern "C" int moe_dispatch(const moe_shape* shape, const int32_t* topk_idx, con
     const int P = s.n_tokens * s.top_k;
     const DispatchPlan plan = dispatch_plan(s.n_tokens, s.n_experts);
     int32_t* counts = nullptr;
-    if (P > kKeysAlone) {
+    if (dispatch_count(P, s.n_experts) == COUNT_LAUNCH) {
         if (!workspace || workspace_bytes < dispatch_scratch_bytes(s.n_tokens, s.n_experts)) return MOE_ERR_WORKSPACE;
         if (!aligned4(workspace)) return MOE_ERR_INVALID;
         counts = static_cast<int32_t*>(workspace);

@@ -4,7 +4,9 @@ import pytest
 import torch
 
 import paper_2503_00245_amd as pkg
+from tests import test_training_gpu as base
 from tests import training_oracle as to
+from tests.rows_cases import ROWS
 from tests.test_training_gpu import dev, dispatched, gen, picks, rnd
 
 pytestmark = pytest.mark.gpu
@@ -26,3 +28,15 @@ def test_rows_of_a_weight_decomposed_layer(flags):
     y = torch.full((T, d), float("nan"), device=dev())
     pkg.moe_collect(shape, rows, inv, gate.to(dev()), None, y)
     to.near(y, to.gather_sum(rows.cpu(), inv.cpu().view(T, k), gate, None, torch.float32), "y")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,d,E,k", ROWS)
+def test_forms_of_dispatch_and_its_gradient(T, d, E, k, dtype):
+    base.test_dispatch_and_its_gradient(T, d, E, k, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,d,E,k", ROWS)
+def test_forms_of_collect_and_its_gradient(T, d, E, k, dtype):
+    base.test_collect_and_its_gradient(T, d, E, k, dtype)

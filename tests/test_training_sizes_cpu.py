@@ -1,10 +1,15 @@
 """What a call around the experts needs is told for every shape that it accepts: sizes of workspaces, and which forms of the kernels the GPU tests reach."""
 import ctypes as C
+import os
+import subprocess
 
 import pytest
 import torch
 
 import paper_2503_00245_amd as pkg
+from paper_2503_00245_amd import build as hip_build
+from tests.rows_cases import ROWS
+from tests.test_training_gpu import SIZES
 
 WORKSPACE = -3
 P = [C.c_void_p(i << 20) for i in range(1, 9)]  # addresses that no launch will see
@@ -43,3 +48,15 @@ def test_sizes_of_dispatch_refuse_and_do_not_fall():
         sizes = [pkg.moe_dispatch_workspace_bytes(pkg.make_shape(t, 64, 136, E, k, rank=64)) for t in [*range(3000), *range(3000, 200000, 97)]]
         assert sizes[0] > 0 and all(a <= b for a, b in zip(sizes, sizes[1:]))
     assert pkg.alloc_dispatch_workspace(pkg.make_shape(0, 64, 136, 4, 2), "cpu").dtype is torch.uint8
+
+
+def test_the_tested_rows_reach_every_form_of_their_kernels(tmp_path):
+    exe = str(tmp_path / "check")
+    subprocess.run(["g++", "-O2", "-std=c++17", "-I", hip_build.CSRC, os.path.join(os.path.dirname(__file__), "rows_plan_check.cpp"), "-o", exe], check=True)
+    plans = {c: tuple(map(int, subprocess.run([exe, *map(str, c)], capture_output=True, text=True, check=True, timeout=60).stdout.split())) for c in ROWS + SIZES}
+    assert {p[:2] for p in plans.values()} == {(w, n) for w in (1, 2, 4) for n in (0, 1, 2, 4, 8)}
+    assert {p[2] for p in plans.values()} == {0, 1, 2}
+    # by ballots, of every number of experts that is counted so: chunks that start within a wave's 64 keys, and keys for more than one wave
+    for E in (1, 2, 3, 4):
+        starts = [[chunk * i % 64 for i in range(chunks)] for c, (_, _, how, chunk, chunks) in plans.items() if how == 0 and c[2] == E and c[0] * c[3] > 64]
+        assert any(any(at) for at in starts), E
