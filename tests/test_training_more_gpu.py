@@ -1,11 +1,13 @@
-"""Layers whose experts have no gradient here, and forms of the row kernels that ordinary sizes do not reach, against the plain implementations in 64 bits
+"""Layers whose experts have no gradient here, and forms of the kernels that ordinary sizes do not reach, against the plain implementations in 64 bits
 (training_oracle)."""
 import pytest
 import torch
 
 import paper_2503_00245_amd as pkg
+from tests import test_block_gpu as block
 from tests import test_training_gpu as base
 from tests import training_oracle as to
+from tests.block_cases import WIDE, WIDE_MANY
 from tests.rows_cases import ROWS
 from tests.test_training_gpu import dev, dispatched, gen, picks, rnd
 
@@ -40,3 +42,22 @@ def test_forms_of_dispatch_and_its_gradient(T, d, E, k, dtype):
 @pytest.mark.parametrize("T,d,E,k", ROWS)
 def test_forms_of_collect_and_its_gradient(T, d, E, k, dtype):
     base.test_collect_and_its_gradient(T, d, E, k, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("what", ["", "pgt"])
+@pytest.mark.parametrize("T,d", WIDE)
+def test_block_of_wide_rows(T, d, what, dtype):
+    block.test_block(T, d, what, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,d", WIDE_MANY)
+def test_wide_rows_do_not_depend_on_the_rows_around_them(T, d, dtype):
+    block.test_rows_do_not_depend_on_the_rows_around_them(T, d, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,d,p", [(3, 10240, 0.1), (2, 20000, 0.3), (2, 32768, 0.5)])
+def test_dropout_of_wide_rows(T, d, p, dtype):
+    block.test_dropout(T, d, p, dtype)
