@@ -110,7 +110,9 @@ MOE_API int moe_expert_ffn_backward(const moe_shape* shape, const moe_weights* w
  * keeps by 65536 / (65536 - r).  Value i is dropped if half i % 8 of Philox4x32-10 (Salmon, Moraes, Dror, Shaw: Parallel random
  * numbers: as easy as 1, 2, 3) is below r, halves counted from the lower one of word 0, with the counter (i / 8, rng[1]), each 64
  * bits, lower half first, and the key rng[0].  The mask is never stored: the backward pass makes it again.  rng [2] uint64 lies on the
- * device, 8-byte aligned, so that a captured graph takes new numbers at every replay; it is read only where r > 0.
+ * device, 8-byte aligned, so that a captured graph takes new numbers at every replay; it is read only where r > 0.  Nothing else enters
+ * the mask: calls of the same numbers drop the same places, so layers and steps whose masks shall not depend on one another need
+ * numbers of their own (another seed, or another offset).
  */
 typedef struct moe_block {
     float eps;                 /* > 0, finite */
@@ -157,7 +159,7 @@ MOE_API int moe_block_norm_backward(const moe_block* block, int32_t n_tokens, in
  *   n_0 = N(x; open_w[0]);  b_l = layer_l(n_l);  x_{l+1}, n_{l+1} by blocks[l] and open_w[l+1] as above;  y = x_{n_layers}
  * the end of a block and the start of the next in one launch.  layers, blocks [n_layers] and open_w [n_layers] (of device pointers)
  * are host arrays; every open_w[l] is needed, and its eps is that of blocks[l] for l = 0 and of blocks[l - 1] after.  A
- * token_gate and an rng are those of their block.  topk_trace [n_layers, T, k] int32 or NULL.  shape.flags' residual bit is
+ * token_gate and an rng are those of their block: with one rng for all blocks every layer drops the same places.  topk_trace [n_layers, T, k] int32 or NULL.  shape.flags' residual bit is
  * refused.  workspace: moe_block_stack_workspace_bytes(shape), 16-byte aligned.
  */
 MOE_API size_t moe_block_stack_workspace_bytes(const moe_shape* shape); /* 0 if invalid */

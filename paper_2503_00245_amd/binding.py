@@ -622,7 +622,8 @@ class Block:
 
 
 def make_block(eps=1e-5, skip_scale=1.0, block_scale=1.0, dropout=0.0, post_w=None, gate=None, token_gate=None, rng=None) -> Block:
-    """post_w, gate f32 [d], token_gate f32 [T], each or None; rng int64 or uint64 [2] (seed, offset) on the device, needed for dropout."""
+    """post_w, gate f32 [d], token_gate f32 [T], each or None; rng int64 or uint64 [2] (seed, offset) on the device, needed for dropout: the
+    mask's only source, so every layer has one of its own, and every step new numbers in it."""
     t = {"post_w": post_w, "gate": gate, "token_gate": token_gate, "rng": rng}
     for name in ("post_w", "gate", "token_gate"):
         if t[name] is not None:

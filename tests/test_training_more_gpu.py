@@ -9,7 +9,7 @@ from tests import test_training_gpu as base
 from tests import training_oracle as to
 from tests.block_cases import WIDE, WIDE_MANY
 from tests.rows_cases import ROWS
-from tests.test_training_gpu import dev, dispatched, gen, picks, rnd
+from tests.test_training_gpu import CODE, DTYPES, dev, dispatched, gen, picks, rnd
 
 pytestmark = pytest.mark.gpu
 
@@ -61,3 +61,57 @@ def test_wide_rows_do_not_depend_on_the_rows_around_them(T, d, dtype):
 @pytest.mark.parametrize("T,d,p", [(3, 10240, 0.1), (2, 20000, 0.3), (2, 32768, 0.5)])
 def test_dropout_of_wide_rows(T, d, p, dtype):
     block.test_dropout(T, d, p, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [1, 33])
+def test_stack_of_blocks_with_dropout(T, dtype):
+    # every block drops by its own numbers, in eager calls and in replays of a graph; blocks with the same numbers drop the same places
+    dt, d, F, E, k, L, p = DTYPES[dtype], 128, 256, 8, 2, 3, 0.25
+    g = gen(T + 40)
+    shape = pkg.make_shape(T, d, F, E, k, act_dtype=CODE[dt])
+    kept = [{n: rnd(g, *s, std=s[-1] ** -0.5, dtype=torch.float32 if n == "router_w" else dt).to(dev())
+             for n, s in (("router_w", (E, d)), ("w_gate", (E, F, d)), ("w_up", (E, F, d)), ("w_down", (E, d, F)))} for _ in range(L)]
+    layers = [pkg.make_weights(w) for w in kept]
+    cfgs = [block.config(g, T, d, w, p) for w in ("pg", "pgt", "")]
+    numbers = [torch.tensor([77, i], device=dev()) for i in range(L)]
+    blocks = [pkg.make_block(**{n: block.on(v) if torch.is_tensor(v) else v for n, v in {**c, "rng": r}.items()}) for c, r in zip(cfgs, numbers)]
+    open_w = [block.on(1 + rnd(g, d, std=0.2)) for _ in range(L)]
+    x = block.on(rnd(g, T, d, dtype=dt))
+    y, ws = torch.empty_like(x), pkg.alloc_block_stack_workspace(shape, dev())
+    lws = pkg.alloc_workspace(shape, dev())
+
+    def one_by_one():
+        cur, masks = x.clone(), []
+        for l in range(L):
+            n, b, nxt = (torch.empty_like(x) for _ in range(3))
+            pkg.moe_block_norm(blocks[max(l - 1, 0)], cur, None, open_w[l], None, n)
+            pkg.moe_forward(shape, layers[l], n, b, None, None, lws)
+            pkg.moe_block_norm(blocks[l], cur, b, None, nxt, None)
+            masks.append(to.kept(T, d, p, numbers[l].tolist()))
+            to.near(nxt, to.block(cfgs[l], cur.cpu(), b.cpu(), masks[-1], dt), "y")
+            cur = nxt
+        return cur, masks
+
+    def run():
+        pkg.moe_block_stack_forward(shape, layers, blocks, open_w, x, y, None, ws)
+    run()
+    want, masks = one_by_one()
+    assert torch.equal(y, want)
+    assert not any(torch.equal(masks[i], masks[j]) for i in range(L) for j in range(i))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for step in range(3):
+        for r in numbers:
+            r[1] += L
+        if step == 2:  # the same numbers for every block
+            for r in numbers:
+                r.copy_(torch.tensor([5, 6]))
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = y.clone()
+        want, masks = one_by_one()
+        assert torch.equal(replayed, want)
+        assert torch.equal(masks[0], masks[1]) == (step == 2)
