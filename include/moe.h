@@ -133,7 +133,9 @@ MOE_API int moe_permute(const moe_shape* shape, const int32_t* topk_idx, int32_t
  * rank > 0 each matrix-vector product is the factored one of Sec. 2.2, Eq. 1 (see
  * moe_weights).  Accumulation is fp32; with bf16 storage the inner activations
  * (the F-wide hidden vector and the rank-r intermediates) are rounded to bf16.
- *   x_perm [P, d] in, y_perm [P, d] out (act_dtype); expert_offsets [E+1] as above.
+ *   x_perm [P, d] in, y_perm [P, d] out (act_dtype); expert_offsets [E+1] as above, or
+ *   ending before P (pairs that are switched off, see moe_dispatch in moe_training.h): rows
+ *   from expert_offsets[E] on are neither read nor written, whatever the experts' form.
  */
 MOE_API int moe_expert_ffn(const moe_shape* shape, const moe_weights* weights, const void* x_perm,
                    const int32_t* expert_offsets, void* y_perm, void* workspace,

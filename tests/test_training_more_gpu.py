@@ -115,3 +115,58 @@ def test_stack_of_blocks_with_dropout(T, dtype):
         want, masks = one_by_one()
         assert torch.equal(replayed, want)
         assert torch.equal(masks[0], masks[1]) == (step == 2)
+
+
+def _factored_forward(x, offsets, w, dtype):
+    """y_perm of the rows that have a group, of experts M v = L (R v) (+ M0 v), with its bound: R v, h and y are rounded to the storage type"""
+    u, live = to.HALF[dtype], offsets[-1]
+    base = "w_gate" in w
+    v, bound = (torch.zeros(live, x.shape[1], dtype=torch.float64, device=x.device) for _ in range(2))
+
+    def product(A, eA, e, right, left, whole):
+        R, L = w[right][e].double(), w[left][e].double()
+        t = A @ R.T
+        et = eA @ R.abs().T + (A.shape[1] + 2) * to.U32 * ((A.abs() + eA) @ R.abs().T)
+        et = et + u * (t.abs() + et)
+        out, size = t @ L.T, (t.abs() + et) @ L.abs().T
+        off = et @ L.abs().T
+        if base:
+            M = w[whole][0].double()
+            out, size, off = out + A @ M.T, size + (A.abs() + eA) @ M.abs().T, off + eA @ M.abs().T
+        return out, off + (A.shape[1] + R.shape[0] + 4) * to.U32 * size
+    for e, (lo, hi) in enumerate(zip(offsets, offsets[1:])):
+        X = x[lo:hi].double()
+        none = torch.zeros_like(X)
+        a, ea = product(X, none, e, "rg", "lg", "w_gate")
+        b, eb = product(X, none, e, "ru", "lu", "w_up")
+        act = a * torch.sigmoid(a)
+        h = act * b
+        eact = 1.1 * ea + act.abs() * (1.5 * a.abs() + 8) * to.U32  # (|silu'| <= 1.1)
+        eh = act.abs() * eb + (b.abs() + eb) * eact + 4 * to.U32 * h.abs()
+        eh = eh + u * (h.abs() + eh)
+        y, ey = product(h, eh, e, "rd", "ld", "w_down")
+        v[lo:hi], bound[lo:hi] = y, ey + u * (y.abs() + ey)
+    return v, bound
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("T,d,F,E,k,r", [(1, 128, 256, 8, 2, 64), (8, 256, 512, 4, 2, 128), (40, 432, 1152, 8, 2, 216), (300, 264, 520, 4, 2, 72), (2000, 136, 264, 8, 2, 40)])
+def test_factored_experts_of_a_batch_with_padding(T, d, F, E, k, r, shared, dtype):
+    # the forward pass of weight-decomposed experts, alone and beside a shared base, on groups that end before the last row
+    dt, g = DTYPES[dtype], gen(T + r)
+    shape = pkg.make_shape(T, d, F, E, k, rank=r, act_dtype=CODE[dt], flags=pkg.FLAG_SHARED_BASE if shared else 0)
+    sizes = {"rg": (E, r, d), "ru": (E, r, d), "lg": (E, F, r), "lu": (E, F, r), "rd": (E, r, F), "ld": (E, d, r)}
+    if shared:
+        sizes.update(w_gate=(1, F, d), w_up=(1, F, d), w_down=(1, d, F))
+    w = {n: rnd(g, *s, std=s[-1] ** -0.5, dtype=dt).to(dev()) for n, s in sizes.items()}
+    for masked in (0.4, 1.0):
+        idx = picks(g, T, k, E, masked)
+        offsets = [0] + torch.bincount(idx[idx >= 0].flatten().long(), minlength=E).cumsum(0).tolist()
+        live = offsets[-1]
+        x = rnd(g, T * k, d, dtype=dt)
+        x[live:] = float("nan")
+        x, y = x.to(dev()), torch.full((T * k, d), -7.0, dtype=dt, device=dev())
+        pkg.moe_expert_ffn(shape, pkg.make_weights(w), x, torch.tensor(offsets, dtype=torch.int32, device=dev()), y, pkg.alloc_workspace(shape, dev()))
+        to.near(y[:live], _factored_forward(x, offsets, w, dt), "y_perm")
+        assert (y[live:] == -7.0).all()
