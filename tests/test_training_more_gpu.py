@@ -170,3 +170,37 @@ def test_factored_experts_of_a_batch_with_padding(T, d, F, E, k, r, shared, dtyp
         pkg.moe_expert_ffn(shape, pkg.make_weights(w), x, torch.tensor(offsets, dtype=torch.int32, device=dev()), y, pkg.alloc_workspace(shape, dev()))
         to.near(y[:live], _factored_forward(x, offsets, w, dt), "y_perm")
         assert (y[live:] == -7.0).all()
+
+
+def _beyond_4_gb(d, F, row_bytes):
+    """Layer of 2^21 pairs of one expert and of two, the data of a few thousand rows alone: those past 2^32 bytes of a tensor of row_bytes a row, and the
+    128 before them.  The others are zeros, which add nothing to the gradients of weights, in any order."""
+    T = 1 << 21
+    first = (1 << 32) // row_bytes - 128
+    assert 2000 < T - first < 40000
+    g = torch.Generator(device=dev())
+    g.manual_seed(d)
+    x, gy = (torch.zeros(T, d, dtype=torch.bfloat16, device=dev()) for _ in range(2))
+    for t in (x, gy):
+        t[first:] = torch.randn(T - first, d, generator=g, device=dev()).bfloat16()
+    w = [(torch.randn(2, *s, generator=g, device=dev()) * s[1] ** -0.5).bfloat16() for s in ((F, d), (F, d), (d, F))]
+    return T, first, x, gy, w
+
+
+@pytest.mark.parametrize("d,F", [(136, 1032), (1032, 136)])
+def test_gradients_of_weights_from_rows_beyond_4_gb(d, F):
+    # h, da and db are wide in the one layer, x and its gradient in the other; the rows that count lie behind 4 GB, in a group that starts there and in one
+    # that starts at the first row
+    T, first, x, gy, w = _beyond_4_gb(d, F, 2 * max(d, F))
+    shape, ws = base.make(T, d, 2, 1, torch.bfloat16, F)
+    weights = pkg.make_weights(dict(zip(("w_gate", "w_up", "w_down"), w)))
+    for offsets in ([0, first, T], [0, T, T]):
+        outs = [torch.full_like(t, float("nan")) for t in (x, *w)]
+        pkg.moe_expert_ffn_backward(shape, weights, x, torch.tensor(offsets, dtype=torch.int32, device=dev()), gy, *outs, ws)
+        e = 1 if offsets[1] == first else 0
+        want = to.experts_grad(x[first:], [0, 0, T - first] if e else [0, T - first, T - first], gy[first:], *w, torch.bfloat16)
+        to.near(outs[0][first:], want[0], "grad_x_perm")
+        assert (outs[0][:first] == 0).all()
+        for name, o, v in zip(("gate", "up", "down"), outs[1:], want[1:]):
+            to.near(o, v, name)
+        del outs
