@@ -7,7 +7,8 @@
  * `stream` without synchronising, statuses found on the host before any launch, nothing allocated or kept,
  * the same bits for the same inputs.  Arrays of int32 and fp32 need 4-byte alignment only, but for post_w, gate and open_w below
  * (16 bytes).  No output may overlap an
- * input or another output unless it is said.  Calls may be captured into graphs.
+ * input or another output unless it is said.  Calls may be captured into graphs.  Non-finite inputs give unspecified results (an
+ * infinite one may be NaN), but what is said to play no part, or not to be read, may hold anything.
  */
 #ifndef MOE_TRAINING_H_
 #define MOE_TRAINING_H_

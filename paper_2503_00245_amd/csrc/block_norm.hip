@@ -1,10 +1,13 @@
 // The block around a layer: its end (norm, gates, dropout, scaled residual) and the start of the next (norm), in one pass over the
 // rows, and the gradient of both in one pass and a small sum over tokens (moe_training.h states them).
 //
-// A row is held in registers, so that every tensor is read once and written once: what bounds both is memory.
+// A row of up to 8192 values is held in registers, so that every tensor is read once and written once: what bounds both is memory.
 // WAVES of a workgroup share a row of up to WAVES * 512 * CHUNKS values: eight values a lane (CHUNKS 1), or sixteen, leave the registers for the weights and the next
 // row.  (With a wave a row of 2048, 32 values a lane, weights read again for every row: 60 us forward, 131 back.)
-// 16384 rows of 2048, bf16, dropout: forward 55 us (268 MB, 4.9 TB/s), back 85 + 5 (403 MB and 19 MB of sums); 2048 rows of 1440 back 15.3 + 4.6.
+// 16384 rows of 2048, bf16, dropout: forward 55 us (268 MB, 4.9 TB/s), back 85 + 5 (403 MB and 19 MB of sums); 2048 rows of 1440 back 15.3 + 4.5.
+// Wider rows, of which sixteen waves leave a lane 128 registers, keep part of the gradient's values in scratch memory: with sums over rows 77 / 329 / 538 registers
+// of two / three / four chunks in fp32, 45 / 196 / 335 in bf16; without sums 0 / 110 / 262 and 0 / 22 / 63.  1024 x 16384 bf16 forward 33 us, back 96 + 8; 512 x 32768
+// back 260 + 17: 201 MB of rows either way, 39 us of a copy.
 #include <algorithm>
 #include <cmath>
 

@@ -18,7 +18,7 @@
 // accumulator registers a lane) or 96 (144), a and b in a first pass over d, dh in a second one.  dh then is never rounded nor
 // stored: as a tensor of its own in bf16 it raised the error of the gradients from 2.3e-3 to 2.9e-3.
 //
-// Measured, 16384 tokens of 2048 / 5632, Zipf loads: a, b, dh 2126 us (1.07 PFLOP/s), weights 1770 (1.28), rows 1234 (1.22); a library product of 8192^3 runs at
+// Measured, 16384 tokens of 2048 / 5632, Zipf loads: a, b, dh 2135 us (1.06 PFLOP/s), weights 1758 (1.29), rows 1222 (1.24); a library product of 8192^3 runs at
 // 1.44.  What is left out in turn (a copy, for timing): without fills 1640 / 1470 / 950 us, without products 1890 / 1513 / 1040.  Fills come at 46 GB/s a CU,
 // bound by how far ahead LDS lets them be asked for (98 GB/s for the same pattern without the schedule), so bytes of fill a
 // product count: a, b, dh of 128 columns at a time need a fifth less of them than of 96 (2370 -> 2140 us).
@@ -273,7 +273,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                 }
             }
         };
-        // the last step of a pass, `left` k-values of which are its own: the others are taken out of A
+        // the last step of a pass, `left` k-values of which are its own: the others are taken out of A (an infinite value of B there makes NaN of
+        // an infinite result: non-finite inputs are unspecified)
         auto clear_others = [&](int left, int phase) INLINE {
 #pragma unroll
             for (int q = 0; q < HS; ++q) {
